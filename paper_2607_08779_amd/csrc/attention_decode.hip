@@ -1,0 +1,427 @@
+// Attention of a few new tokens of each request over the paged cache, with a prefix that all
+// requests share (see include/ssq_attention.h).
+//
+// The cache is read once, and its bytes are the floor.  Two kinds of workgroups share one
+// launch, and a second launch joins what they found, where there is more than one part:
+//
+// * wide: 128 query rows (all requests' new tokens and the group's heads) against a stretch
+//   of the shared prefix, 64 keys at a time through two stages of LDS that the four
+//   wavefronts share.
+// * narrow: up to 32 query rows (one request's; or all, against the prefix, where they are so
+//   few) against a stretch of keys that the four wavefronts take 32 at a time, each through
+//   LDS of its own and without barriers: the next keys are loaded as soon as the scores of
+//   these are formed, the next values after the product.  Rows beside the used ones
+//   cost nothing that is scarce here.
+//
+// Parts leave O unnormalised in binary32 with its reference and sum, and are joined as
+//   out = sum_s 2^(m_s - M) O_s / sum_s 2^(m_s - M) l_s,   M = max_s m_s.
+#include <algorithm>
+
+#include "attention_tiles.h"
+
+namespace ssq {
+namespace attention {
+namespace {
+
+constexpr int kWaves = 4, kThreads = 64 * kWaves, kWideRows = 32 * kWaves, kWideKeys = 64, kNarrowRows = 32;
+constexpr int kNarrowKeys = 32 * kWaves;              // keys that a narrow workgroup takes at a time
+constexpr int kMaxParts = 64;
+
+enum Share : int { kShareNone = 0, kShareWide, kShareNarrow };
+
+struct Plan {
+  int group;             // query heads of a key/value head
+  int rows;              // requests * fresh * group: rows of a key/value head
+  int share;             // how the prefix is taken
+  int prefix_tiles, prefix_parts;
+  int own_tiles, own_parts;
+  int64_t line_rows;     // requests * fresh * q_heads: rows of out
+  int parts() const { return own_parts + (share != kShareNone ? prefix_parts : 0); }
+  int64_t prefix_groups() const { return share != kShareNone ? (int64_t)prefix_tiles * prefix_parts : 0; }
+};
+
+struct Parts {           // of every row: [part][row] and [part][row][D]
+  float2* ml;            // null: one part, straight to out
+  float* o;
+};
+
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+Plan make_plan(int64_t requests, int fresh, int q_heads, int kv_heads, int64_t max_len, int64_t prefix, bool split) {
+  Plan p = {};
+  p.group = q_heads / kv_heads;
+  p.rows = (int)(requests * fresh * p.group);
+  p.line_rows = requests * fresh * q_heads;
+  p.own_tiles = (int)ceil_div((int64_t)fresh * p.group, kNarrowRows);
+  p.own_parts = 1;
+  p.share = kShareNone;
+  if (!split) return p;
+  constexpr int64_t kGroups = 512;       // two workgroups for each of 256 CUs
+  prefix = std::min(prefix, max_len);
+  if (requests > 1 && prefix > 0) {
+    p.share = p.rows > kNarrowRows ? kShareWide : kShareNarrow;
+    p.prefix_tiles = p.share == kShareWide ? (int)ceil_div(p.rows, kWideRows) : 1;
+    p.prefix_parts = (int)std::clamp(ceil_div(kGroups, (int64_t)p.prefix_tiles * kv_heads), (int64_t)1,
+                                     std::min<int64_t>(kMaxParts / 2, ceil_div(prefix, 256)));
+  } else {
+    prefix = 0;
+  }
+  p.own_parts = (int)std::clamp(ceil_div(kGroups, requests * kv_heads * p.own_tiles), (int64_t)1,
+                                std::min<int64_t>(kMaxParts / 2, std::max<int64_t>(1, ceil_div(max_len - prefix, 256))));
+  return p;
+}
+
+// Rows of this wavefront: lane's column, where it goes and the last key it sees.
+struct Row {
+  bool present;
+  int64_t line;          // row of q and out
+  int column;            // head
+  int last;
+};
+
+// The pages of one table row, and the descriptors of 16 keys in them.
+// The entry is read through the constant address space: a scalar load, which does not wait
+// behind the loads of keys and values in flight as a vector load's result would.
+struct Pages {
+  const int32_t* row;
+  template <typename T>
+  __device__ __forceinline__ bool find(const Cache<T>& c, int j, int64_t* page) const {
+    typedef const __attribute__((address_space(4))) int32_t* uniform_ptr;
+    *page = ((uniform_ptr)row)[j >> c.page_shift];
+    return (uint64_t)*page < (uint64_t)c.pages;
+  }
+};
+
+template <typename T, int D>
+__device__ __forceinline__ int64_t group_offset(const Decode<T>& a, int head, int64_t page, int j) {
+  return (((page * a.kv_heads + head) << a.cache.page_shift) + (j & ((1 << a.cache.page_shift) - 1))) * D;
+}
+
+__device__ __forceinline__ int wave_min(int v) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v = min(v, __shfl_xor(v, o, 64));
+  return __builtin_amdgcn_readfirstlane(v);
+}
+
+template <typename T>
+__device__ __forceinline__ int request_len(const Decode<T>& a, int request) {
+  const int64_t room = min(a.max_len, a.table_stride << a.cache.page_shift);
+  return (int)min((int64_t)max(a.lens[request], 0), room);
+}
+
+// Four consecutive outputs of a row, of one part or of all.
+template <typename T, int D>
+__device__ __forceinline__ void put(const Decode<T>& a, const Plan& p, const Parts& parts, int part, const Row& row,
+                                    int at, f32x4 o, float m, float l) {
+  if (parts.ml == nullptr) {
+    const float by = l != 0.0f ? 1.0f / l : 0.0f;
+    T* to = a.out.p + row.line * a.out.stride + row.column * D + at;
+    if constexpr (sizeof(T) == 2) *reinterpret_cast<u32x2*>(to) = u32x2{pack_bf16x2(o[0] * by, o[1] * by), pack_bf16x2(o[2] * by, o[3] * by)};
+    else *reinterpret_cast<f32x4*>(to) = f32x4{o[0] * by, o[1] * by, o[2] * by, o[3] * by};
+  } else {
+    const int64_t r = part * p.line_rows + row.line * a.q_heads + row.column;
+    *reinterpret_cast<f32x4*>(parts.o + r * D + at) = o;
+    if (at == 0) parts.ml[r] = float2{m, l};
+  }
+}
+
+template <typename T, int D>
+__device__ void wide(const Decode<T>& a, const Plan& p, const Parts& parts, int head, int tile, int part, uint8_t* const (&lds)[4],
+                     int* spoiled) {
+  using S = Shape<T, D>;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int prefix = (int)min(a.prefix, min(a.max_len, a.table_stride << a.cache.page_shift));
+  const int per = ((prefix + p.prefix_parts - 1) / p.prefix_parts + kWideKeys - 1) / kWideKeys * kWideKeys;
+  const int begin = min(part * per, prefix), end = min(begin + per, prefix);
+  const int index = tile * kWideRows + 32 * wave + (lane & 31);
+  Row row;
+  row.present = index < p.rows;
+  const int line = index / p.group, request = line / a.fresh;
+  row.line = line;
+  row.column = head * p.group + index - line * p.group;
+  row.last = row.present ? min(request_len(a, request) - a.fresh + (line - request * a.fresh), prefix - 1) : -1;
+  const int wave_first = wave_min(row.present ? row.last : 0x7fffffff), wave_last = -wave_min(-row.last);
+
+  Rows32<T, D> r;
+  r.load_query(a.q.p + row.line * a.q.stride + row.column * D, row.present, lane);
+  const Loader<T, D> load(lane, S::kRow);
+  const float scale = a.scale * kLog2e;
+  const Pages pages = {a.table};
+  auto fill = [&](int j, uint8_t* k, uint8_t* v) {
+    const int first = j + 16 * wave, count = min(end - first, 16);
+    int64_t page = 0;
+    const bool here = count > 0 && pages.find(a.cache, first, &page);
+    const int64_t at = here ? group_offset<T, D>(a, head, page, first) : 0;
+    const uint32_t bytes = here ? (uint32_t)(count * S::kRow) : 0u;
+    load.keys(make_rsrc(a.cache.k + at, bytes), k + wave * S::kGroup);
+    load.values(make_rsrc(a.cache.v + at, bytes), v + wave * S::kGroup);
+  };
+  auto use = [&](int j, const uint8_t* k, const uint8_t* v, bool careful) {
+    if (j > wave_last) return;
+    uint32_t absent = 0;
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      int64_t page;
+      if (j + 16 * g < end && !pages.find(a.cache, j + 16 * g, &page)) absent |= 1u << g;
+    }
+    r.template attend<2>(k, v, j + kWideKeys - 1 > wave_first || absent != 0, 0, min(row.last, end - 1) - j, absent, scale, careful, lane);
+  };
+  if (threadIdx.x == 0) *spoiled = 0;
+  for (bool careful = false;; careful = true) {
+    r.start(lane);
+    if (begin < end) fill(begin, lds[0], lds[1]);
+    for (int j = begin; j < end; j += 2 * kWideKeys) {
+      wait_vmcnt<0>();
+      lds_barrier();
+      if (j + kWideKeys < end) fill(j + kWideKeys, lds[2], lds[3]);
+      use(j, lds[0], lds[1], careful);
+      if (j + kWideKeys >= end) break;
+      wait_vmcnt<0>();
+      lds_barrier();
+      if (j + 2 * kWideKeys < end) fill(j + 2 * kWideKeys, lds[0], lds[1]);
+      use(j + kWideKeys, lds[2], lds[3], careful);
+    }
+    if (careful) break;
+    __syncthreads();
+    if (row.present && r.spoiled()) *spoiled = 1;
+    __syncthreads();
+    if (*spoiled == 0) break;
+  }
+  const float l = sum_across(r.l);
+  if (!row.present) return;
+#pragma unroll
+  for (int t = 0; t < S::kOut; ++t)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      put<T, D>(a, p, parts, part, row, 32 * t + 8 * i + 4 * (lane / 32), f32x4{r.o[t][4 * i], r.o[t][4 * i + 1], r.o[t][4 * i + 2], r.o[t][4 * i + 3]}, r.m, l);
+}
+
+// Rows `tile0` ... of `request` (of all requests if it is negative) against keys
+// [begin[s], end[s]) of the table rows `pages[s]`.
+template <typename T, int D>
+__device__ void narrow(const Decode<T>& a, const Plan& p, const Parts& parts, int head, int request, int index0,
+                       const Pages (&pages)[2], const int (&begin)[2], const int (&end)[2], int part, uint8_t* lds, float2* ml) {
+  using S = Shape<T, D>;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int rows = request < 0 ? p.rows : a.fresh * p.group;
+  auto find_row = [&](int n) {
+    Row row;
+    const int index = index0 + n, token = index / p.group;
+    row.present = index < rows;
+    const int of = request < 0 ? token / a.fresh : request;
+    row.line = request < 0 ? token : (int64_t)request * a.fresh + token;
+    row.column = head * p.group + index - token * p.group;
+    row.last = row.present ? request_len(a, of) - a.fresh + (int)(row.line - (int64_t)of * a.fresh) : -1;
+    return row;
+  };
+  const Row row = find_row(lane & 31);
+  const int wave_first = wave_min(row.present ? row.last : 0x7fffffff);
+
+  Rows32<T, D> r;
+  r.load_query(a.q.p + row.line * a.q.stride + row.column * D, row.present, lane);
+  const Loader<T, D> load(lane, S::kRow);
+  const float scale = a.scale * kLog2e;
+  uint8_t *k = lds + wave * 4 * S::kGroup, *v = k + 2 * S::kGroup;
+  for (bool careful = false;; careful = true) {
+    r.start(lane);
+#pragma unroll 1
+    for (int s = 0; s < 2; ++s) {
+      const int lo = s == 0 ? begin[0] : begin[1], hi = s == 0 ? end[0] : end[1];
+      const Pages of = {s == 0 ? pages[0].row : pages[1].row};
+      if (lo >= hi) continue;
+      struct Group {
+        int64_t at;
+        uint32_t bytes;
+        bool absent;
+      };
+      auto find = [&](int first) {                       // 16 keys from a multiple of 16 on
+        Group g = {0, 0u, false};
+        const int count = min(hi - first, 16);
+        if (count > 0) {
+          int64_t page;
+          const bool here = of.find(a.cache, first, &page);
+          g.absent = !here;
+          if (here) g.at = group_offset<T, D>(a, head, page, first), g.bytes = (uint32_t)(count * S::kRow);
+        }
+        return g;
+      };
+      int j = (lo & ~15) + 32 * wave;
+      Group now[2] = {find(j), find(j + 16)};
+#pragma unroll
+      for (int g = 0; g < 2; ++g) load.keys(make_rsrc(a.cache.k + now[g].at, now[g].bytes), k + g * S::kGroup, lo - (j + 16 * g));
+#pragma unroll
+      for (int g = 0; g < 2; ++g) load.values(make_rsrc(a.cache.v + now[g].at, now[g].bytes), v + g * S::kGroup, lo - (j + 16 * g));
+      for (; j < hi; j += kNarrowKeys) {
+        const int next_j = j + kNarrowKeys;
+        const Group next[2] = {find(next_j), find(next_j + 16)};
+        const uint32_t absent = (now[0].absent ? 1u : 0u) | (now[1].absent ? 2u : 0u);
+        const bool edge = j + 31 > min(wave_first, hi - 1) || j < lo || absent != 0;
+        landed<2 * S::kLoads>();
+        f32x16 x[1];
+        r.x.scores(k, x[0]);
+        have_read();
+#pragma unroll
+        for (int g = 0; g < 2; ++g) load.keys(make_rsrc(a.cache.k + next[g].at, next[g].bytes), k + g * S::kGroup, 0);
+        if (edge) Rows32<T, D>::template mask<1>(x, lo - j, min(row.last, hi - 1) - j, absent, lane);
+        typename Products<T, D>::template Weights<1> w;
+        r.template weights<1>(x, scale, w);
+        landed<2 * S::kLoads>();
+        r.template add<1>(v, w, edge && careful, min(row.last, hi - 1) - j, lane);
+        have_read();
+#pragma unroll
+        for (int g = 0; g < 2; ++g) load.values(make_rsrc(a.cache.v + next[g].at, next[g].bytes), v + g * S::kGroup, 0);
+        now[0] = next[0];
+        now[1] = next[1];
+      }
+      landed<0>();
+    }
+    if (careful || __builtin_amdgcn_ballot_w64(row.present && r.spoiled()) == 0) break;
+  }
+  // the four wavefronts' parts, through LDS, 16-byte pieces swizzled by row
+  constexpr int kPieces = D / 4;
+  const float l = sum_across(r.l);
+  __syncthreads();
+  f32x4* const o = reinterpret_cast<f32x4*>(lds);
+  const int n = lane & 31, count = min(rows - index0, kNarrowRows);
+  if (n < count) {
+#pragma unroll
+    for (int t = 0; t < S::kOut; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        o[(wave * 32 + n) * kPieces + ((8 * t + 2 * i + lane / 32) ^ (n % kPieces))] = f32x4{r.o[t][4 * i], r.o[t][4 * i + 1], r.o[t][4 * i + 2], r.o[t][4 * i + 3]};
+    if (lane < 32) ml[wave * 32 + n] = float2{r.m, l};
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < count * kPieces; i += kThreads) {
+    const int at = i % kPieces, of = i / kPieces;
+    float m = ml[of].x, sum = 0.0f;
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) m = fmaxf(m, ml[w * 32 + of].x);
+    f32x4 all = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      const float2 x = ml[w * 32 + of];
+      if (x.y == 0.0f) continue;
+      const float by = __builtin_amdgcn_exp2f(x.x - m);
+      const f32x4 y = o[(w * 32 + of) * kPieces + (at ^ (of % kPieces))];
+      sum = __builtin_fmaf(by, x.y, sum);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) all[e] = __builtin_fmaf(by, y[e], all[e]);
+    }
+    put<T, D>(a, p, parts, part, find_row(of), 4 * at, all, m, sum);
+  }
+}
+
+template <typename T, int D>
+__global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void decode_kernel(const Decode<T> a, const Plan p, const Parts parts, int prefix_blocks) {
+  constexpr int kTile = 64 * Shape<T, D>::kRow;
+  __shared__ __align__(1024) uint8_t lds[4 * kTile];
+  __shared__ float2 ml[kWaves * 32];
+  __shared__ int spoiled;
+  const int block = (int)blockIdx.x;
+  const int prefix = (int)min(a.prefix, min(a.max_len, a.table_stride << a.cache.page_shift));
+  if (block < prefix_blocks) {
+    const int head = block % a.kv_heads, i = block / a.kv_heads, tile = i % p.prefix_tiles, part = i / p.prefix_tiles;
+    if (p.share == kShareWide) {
+      uint8_t* const stages[4] = {lds, lds + kTile, lds + 2 * kTile, lds + 3 * kTile};
+      wide<T, D>(a, p, parts, head, tile, part, stages, &spoiled);
+    } else {
+      const int per = ((prefix + p.prefix_parts - 1) / p.prefix_parts + kNarrowKeys - 1) / kNarrowKeys * kNarrowKeys;
+      const Pages pages[2] = {{a.table}, {a.table}};
+      const int begin[2] = {min(part * per, prefix), 0}, end[2] = {min((part + 1) * per, prefix), 0};
+      narrow<T, D>(a, p, parts, head, -1, 0, pages, begin, end, part, lds, ml);
+    }
+  } else {
+    const int i0 = block - prefix_blocks, head = i0 % a.kv_heads;
+    int i = i0 / a.kv_heads;
+    const int part = i % p.own_parts;
+    i /= p.own_parts;
+    const int tile = i % p.own_tiles, request = i / p.own_tiles;
+    const int len = request_len(a, request), from = min(p.share != kShareNone ? prefix : 0, len);
+    const int per = ((len - from + p.own_parts - 1) / p.own_parts + kNarrowKeys - 1) / kNarrowKeys * kNarrowKeys;
+    const int lo = min(from + part * per, len), hi = min(lo + per, len);
+    // what lies in the prefix comes from the first request's pages, shared or not
+    const Pages pages[2] = {{a.table}, {a.table + request * a.table_stride}};
+    const int begin[2] = {lo, max(lo, prefix)}, end[2] = {min(hi, prefix), hi};
+    narrow<T, D>(a, p, parts, head, request, tile * kNarrowRows, pages, begin, end, p.share != kShareNone ? p.prefix_parts + part : part, lds, ml);
+  }
+}
+
+// One row of out from its parts, a wavefront each.
+template <typename T, int D>
+__global__ __launch_bounds__(kThreads) void join_kernel(const Decode<T> a, int64_t line_rows, int count, const Parts parts) {
+  constexpr int E = D / 64;
+  const int lane = threadIdx.x & 63;
+  const int64_t row = (int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6);
+  if (row >= line_rows) return;
+  const float2 x = lane < count ? parts.ml[lane * line_rows + row] : float2{-FLT_MAX, 0.0f};
+  float m = x.y != 0.0f ? x.x : -FLT_MAX;
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+  const float by = x.y != 0.0f ? __builtin_amdgcn_exp2f(x.x - m) : 0.0f;
+  float l = by * x.y;
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) l += __shfl_xor(l, o, 64);
+  float sum[E] = {};
+  for (int s = 0; s < count; ++s) {
+    const float w = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(by), s));
+    if (__uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x.y), s)) == 0.0f) continue;
+    const float* o = parts.o + (s * line_rows + row) * D + E * lane;
+#pragma unroll
+    for (int e = 0; e < E; ++e) sum[e] = __builtin_fmaf(w, o[e], sum[e]);
+  }
+  const float inv = l != 0.0f ? 1.0f / l : 0.0f;
+  const int64_t line = row / a.q_heads;
+  T* out = a.out.p + line * a.out.stride + (row - line * a.q_heads) * D + E * lane;
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    if constexpr (sizeof(T) == 2) out[e] = f32_to_bf16_bits(sum[e] * inv);
+    else out[e] = sum[e] * inv;
+  }
+}
+
+size_t part_bytes(const Plan& p, int head_dim) {
+  return p.parts() > 1 ? (size_t)p.parts() * (size_t)p.line_rows * (8 + 4 * (size_t)head_dim) : 0;
+}
+
+template <typename T, int D>
+hipError_t launch(const Decode<T>& a, void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  Plan p = make_plan(a.requests, a.fresh, a.q_heads, a.kv_heads, a.max_len, a.prefix, true);
+  size_t need = part_bytes(p, D);
+  if (need > 0 && (workspace == nullptr || workspace_bytes < need)) {
+    p = make_plan(a.requests, a.fresh, a.q_heads, a.kv_heads, a.max_len, a.prefix, false);
+    need = 0;
+  }
+  Parts parts = {nullptr, nullptr};
+  if (need > 0) {
+    parts.o = static_cast<float*>(workspace);
+    parts.ml = reinterpret_cast<float2*>(parts.o + (size_t)p.parts() * p.line_rows * D);
+  }
+  const int64_t prefix_blocks = p.prefix_groups() * a.kv_heads;
+  const int64_t blocks = prefix_blocks + a.requests * p.own_tiles * p.own_parts * a.kv_heads;
+  decode_kernel<T, D><<<dim3((unsigned)blocks), kThreads, 0, stream>>>(a, p, parts, (int)prefix_blocks);
+  if (need > 0) join_kernel<T, D><<<dim3((unsigned)ceil_div(p.line_rows, kWaves)), kThreads, 0, stream>>>(a, p.line_rows, p.parts(), parts);
+  return hipGetLastError();
+}
+
+}  // namespace
+}  // namespace attention
+
+size_t attention_decode_workspace_bytes(int64_t requests, int fresh, int q_heads, int kv_heads, int head_dim,
+                                        int64_t max_len, int64_t prefix) {
+  return attention::part_bytes(attention::make_plan(requests, fresh, q_heads, kv_heads, max_len, prefix, true), head_dim);
+}
+
+template <typename T>
+static hipError_t launch_by_dim(const Decode<T>& a, int head_dim, void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  return head_dim == 64 ? attention::launch<T, 64>(a, workspace, workspace_bytes, stream)
+                        : attention::launch<T, 128>(a, workspace, workspace_bytes, stream);
+}
+hipError_t launch_attention_decode(const Decode<uint16_t>& a, int head_dim, void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  return launch_by_dim(a, head_dim, workspace, workspace_bytes, stream);
+}
+hipError_t launch_attention_decode(const Decode<float>& a, int head_dim, void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  return launch_by_dim(a, head_dim, workspace, workspace_bytes, stream);
+}
+
+}  // namespace ssq

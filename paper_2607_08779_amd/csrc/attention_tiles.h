@@ -1,0 +1,396 @@
+// Attention of 32 query rows against tiles of 32 keys on the matrix cores, in bf16 or binary32:
+// the parts that the prompt and the decode kernels are made of.
+//
+// A wavefront holds 32 query rows (a row is one token's one head; the heads of a group share
+// their keys, so rows of several heads and tokens go together).  Scores are formed
+// transposed, S^T = K Q^T, so that a lane holds one query (column lane % 32) and half of a
+// tile's keys: key 8 (i / 4) + 4 (lane / 32) + i % 4 in register i.  The softmax then runs
+// inside a lane, with one exchange between lane and lane ^ 32 for the maximum of a tile, and
+// its weights are already the B operand of O^T += V^T P^T, keys permuted within 16 (the
+// order of a sum's terms is free): slots 0-3 of a lane are keys 4 h + (0..3), slots 4-7
+// keys 8 + 4 h + (0..3).  V^T is read from row-major V in LDS by transposing reads in that order.
+//
+// O and the sum of the weights are relative to a running reference m (log2 units): weights
+// are 2^(scale log2(e) s - m).  m only moves, and O is only rescaled, when a tile's maximum
+// exceeds it by more than kSlack: weights stay below 2^kSlack, far from any overflow, and
+// their relative rounding to bf16 does not depend on m.
+//
+// Both tiles live in LDS as rows of D elements, 16-byte chunks XOR-swizzled so that the 16 lanes
+// an access serves at once spread over all banks; the swizzle is applied to the global address
+// of a direct-to-LDS load, whose LDS side is linear.
+#pragma once
+
+#include <float.h>
+
+#include "attention_internal.h"
+#include "mfma_dequant.h"
+
+namespace ssq {
+namespace attention {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4* lds_s16x4;
+typedef __attribute__((address_space(3))) void* lds_void;
+
+constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kSlack = 8.0f;
+constexpr uint32_t kNowhere = 0x80000000u;      // past every descriptor's bytes: loads zeros
+
+template <typename T, int D>
+struct Shape {
+  static constexpr int kRow = (int)sizeof(T) * D;             // bytes of a key's row
+  static constexpr int kChunks = kRow / 16;                   // 16-byte chunks of it
+  static constexpr int kOut = D / 32;                         // MFMA tiles of outputs along the head
+  static constexpr int kGroup = 16 * kRow;                    // bytes of 16 keys, the unit of loading
+  static constexpr int kLoads = kGroup / 1024;                // 1 KB loads of a wavefront for it
+  static constexpr int kLoadRows = 1024 / kRow;
+  static constexpr int kQuery = D / 2;                        // a lane's half of a query, in elements
+};
+
+// XOR of a row's chunk numbers in LDS: 16 rows at one chunk (keys), and 4 rows at a run of
+// 64 bytes (bf16 values), then touch every bank once.
+template <typename T, int D>
+__device__ __forceinline__ int key_swizzle(int row) { return sizeof(T) == 2 && D == 64 ? (row >> 1) & 7 : row & 15; }
+template <typename T, int D>
+__device__ __forceinline__ int value_swizzle(int row) {
+  return sizeof(T) == 4 ? 0 : D == 128 ? 4 * (row & 3) : 4 * ((row >> 1) & 1);
+}
+
+__device__ __forceinline__ float max_across(float v) {       // of lane and lane ^ 32
+  const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(s[0]), __uint_as_float(s[1]));
+}
+__device__ __forceinline__ float sum_across(float v) {
+  const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(s[0]) + __uint_as_float(s[1]);
+}
+
+// Every load but the last N has landed, for this wavefront: what it reads from LDS is read after.
+template <int N>
+__device__ __forceinline__ void landed() {
+  wait_vmcnt<N>();
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
+// This wavefront's LDS reads have returned: what they read may be loaded over.
+__device__ __forceinline__ void have_read() {
+  __builtin_amdgcn_s_waitcnt(0xC07F);             // lgkmcnt(0)
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+// Loads of 16 keys into LDS by one wavefront: `stride` bytes between rows, row0 the first row of
+// the group that is to be loaded (earlier ones become zeros, as do rows past the descriptor's
+// bytes; the whole offset is the lane's, so that all of it counts in that check).
+template <typename T, int D>
+struct Loader {
+  using S = Shape<T, D>;
+  uint32_t k_off[S::kLoads], v_off[S::kLoads];
+  int row;
+  __device__ __forceinline__ Loader(int lane, uint32_t stride) {
+    row = lane / S::kChunks;
+#pragma unroll
+    for (int i = 0; i < S::kLoads; ++i) {
+      const int r = row + i * S::kLoadRows, c = lane % S::kChunks;
+      k_off[i] = (uint32_t)r * stride + 16u * (uint32_t)(c ^ key_swizzle<T, D>(r));
+      v_off[i] = (uint32_t)r * stride + 16u * (uint32_t)(c ^ value_swizzle<T, D>(r));
+    }
+  }
+  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t r, uint8_t* to, const uint32_t (&off)[S::kLoads], int row0) const {
+#pragma unroll
+    for (int i = 0; i < S::kLoads; ++i)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void)(to + 1024 * i), 16,
+                                               (int)(row + i * S::kLoadRows < row0 ? kNowhere : off[i]), 0, 0, 0);
+  }
+  __device__ __forceinline__ void keys(__amdgpu_buffer_rsrc_t r, uint8_t* to, int row0 = 0) const { load(r, to, k_off, row0); }
+  __device__ __forceinline__ void values(__amdgpu_buffer_rsrc_t r, uint8_t* to, int row0 = 0) const { load(r, to, v_off, row0); }
+};
+
+// The products of 32 query rows with tiles of 32 keys: what depends on the element type.
+template <typename T, int D>
+struct Products;
+
+template <int D>
+struct Products<uint16_t, D> {
+  using S = Shape<uint16_t, D>;
+  static constexpr int kSteps = D / 16;
+  bf16x8 q[kSteps];
+  uint32_t k_at[kSteps], v_at[S::kOut];
+  template <int KT>
+  struct Weights {
+    u32x4 w[2 * KT];               // B operands of 16 keys each
+  };
+
+  __device__ __forceinline__ void start(int lane) {
+    const int h = lane / 32;
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) k_at[s] = (uint32_t)((lane & 31) * S::kRow + 16 * ((2 * s + h) ^ key_swizzle<uint16_t, D>(lane & 31)));
+    const int i = lane & 15;
+#pragma unroll
+    for (int t = 0; t < S::kOut; ++t)
+      v_at[t] = (uint32_t)((4 * h + i / 4) * S::kRow + 16 * ((4 * t + 2 * ((lane / 16) & 1) + (i & 3) / 2) ^ value_swizzle<uint16_t, D>(i / 4)) + 8 * (i & 1));
+  }
+  __device__ __forceinline__ void load_query(const uint16_t* row, bool present, int lane) {
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) {
+      u32x4 d = {0u, 0u, 0u, 0u};
+      if (present) d = *reinterpret_cast<const u32x4*>(row + 16 * s + 8 * (lane / 32));
+      q[s] = __builtin_bit_cast(bf16x8, d);
+    }
+  }
+  __device__ __forceinline__ void scores(const uint8_t* keys, f32x16& s) const {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[i] = 0.0f;
+#pragma unroll
+    for (int k = 0; k < kSteps; ++k)
+      s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(keys + k_at[k]), q[k], s, 0, 0, 0);
+  }
+  // Weights w[2 i], w[2 i + 1] of a lane's half of tile kt, rounded to bf16.
+  template <int KT>
+  static __device__ __forceinline__ void set(Weights<KT>& p, int kt, int i, float a, float b) {
+    p.w[2 * kt + i / 4][i % 4] = pack_bf16x2(a, b);
+  }
+  // V^T of 16 keys (chunk c of the tile) and 32 outputs (tile t), as an A operand.
+  __device__ __forceinline__ bf16x8 value(const uint8_t* values, int c, int t) const {
+    s16x4 d[2];
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+      d[s] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(values + v_at[t] + (16 * c + 8 * s) * S::kRow));
+    const auto lo = __builtin_bit_cast(u32x2, d[0]), hi = __builtin_bit_cast(u32x2, d[1]);
+    return __builtin_bit_cast(bf16x8, u32x4{lo.x, lo.y, hi.x, hi.y});
+  }
+  template <int KT>
+  __device__ __forceinline__ void accumulate(const uint8_t* values, const Weights<KT>& p, f32x16 (&o)[S::kOut]) const {
+#pragma unroll
+    for (int c = 0; c < 2 * KT; ++c)
+#pragma unroll
+      for (int t = 0; t < S::kOut; ++t)
+        o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(value(values, c, t), __builtin_bit_cast(bf16x8, p.w[c]), o[t], 0, 0, 0);
+  }
+  // One key's weight for this lane's column, and four of its values.
+  template <int KT>
+  static __device__ __forceinline__ float weight_of(const Weights<KT>& p, int key) {
+    const int slot = (key % 16) / 8 * 4 + key % 4, word = key / 16 * 4 + slot / 2;
+    uint32_t d = 0;
+#pragma unroll
+    for (int i = 0; i < 8 * KT; ++i) d = i == word ? p.w[i / 4][i % 4] : d;
+    const auto s = __builtin_amdgcn_permlane32_swap(d, d, false, false);
+    d = (key / 4) % 2 ? s[1] : s[0];
+    return slot % 2 ? bf16_hi(d) : bf16_lo(d);
+  }
+  static __device__ __forceinline__ f32x4 values_of(const uint8_t* values, int key, int at) {
+    const u32x2 d = *reinterpret_cast<const u32x2*>(values + key * S::kRow + 16 * (at / 8 ^ value_swizzle<uint16_t, D>(key)) + 2 * (at % 8));
+    return f32x4{bf16_lo(d.x), bf16_hi(d.x), bf16_lo(d.y), bf16_hi(d.y)};
+  }
+};
+
+// Binary32: the same tiles on v_mfma_f32_32x32x2_f32 (one key or dimension of each half a
+// step).  The dimensions of a head are taken in the order in which a lane reads them, 16
+// bytes at a time: step 4 u + e multiplies dimensions 8 u + e and 8 u + 4 + e.
+template <int D>
+struct Products<float, D> {
+  using S = Shape<float, D>;
+  float q[D / 2];
+  uint32_t k_base, v_base;
+  int k_swz;
+  template <int KT>
+  struct Weights {
+    f32x16 w[KT];
+  };
+
+  __device__ __forceinline__ void start(int lane) {
+    k_base = (uint32_t)((lane & 31) * S::kRow);
+    k_swz = key_swizzle<float, D>(lane & 31) ^ (lane / 32);
+    v_base = (uint32_t)(4 * (lane / 32) * S::kRow + 4 * (lane & 31));
+  }
+  __device__ __forceinline__ void load_query(const float* row, bool present, int lane) {
+#pragma unroll
+    for (int u = 0; u < D / 8; ++u) {
+      f32x4 d = {0.0f, 0.0f, 0.0f, 0.0f};
+      if (present) d = *reinterpret_cast<const f32x4*>(row + 8 * u + 4 * (lane / 32));
+#pragma unroll
+      for (int e = 0; e < 4; ++e) q[4 * u + e] = d[e];
+    }
+  }
+  __device__ __forceinline__ void scores(const uint8_t* keys, f32x16& s) const {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[i] = 0.0f;
+#pragma unroll
+    for (int u = 0; u < D / 8; ++u) {
+      const f32x4 d = *reinterpret_cast<const f32x4*>(keys + k_base + 16 * ((2 * u) ^ k_swz));
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_32x32x2f32(d[e], q[4 * u + e], s, 0, 0, 0);
+    }
+  }
+  template <int KT>
+  static __device__ __forceinline__ void set(Weights<KT>& p, int kt, int i, float a, float b) {
+    p.w[kt][2 * i] = a;
+    p.w[kt][2 * i + 1] = b;
+  }
+  template <int KT>
+  __device__ __forceinline__ void accumulate(const uint8_t* values, const Weights<KT>& p, f32x16 (&o)[S::kOut]) const {
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+#pragma unroll
+        for (int t = 0; t < S::kOut; ++t)
+          o[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(*reinterpret_cast<const float*>(values + v_base + (32 * kt + 8 * (i / 4) + i % 4) * S::kRow + 128 * t),
+                                                      p.w[kt][i], o[t], 0, 0, 0);
+  }
+  template <int KT>
+  static __device__ __forceinline__ float weight_of(const Weights<KT>& p, int key) {
+    const int reg = key / 32 * 16 + (key % 32) / 8 * 4 + key % 4;
+    float w = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 16 * KT; ++i) w = i == reg ? p.w[i / 16][i % 16] : w;
+    const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(w), __float_as_uint(w), false, false);
+    return __uint_as_float((key / 4) % 2 ? s[1] : s[0]);
+  }
+  static __device__ __forceinline__ f32x4 values_of(const uint8_t* values, int key, int at) {
+    return *reinterpret_cast<const f32x4*>(values + key * S::kRow + 4 * at);
+  }
+};
+
+// 32 query rows of a wavefront and what they have gathered so far.
+template <typename T, int D>
+struct Rows32 {
+  using S = Shape<T, D>;
+  using P = Products<T, D>;
+  P x;
+  f32x16 o[S::kOut];
+  float m, l;                     // reference (log2 units) and this lane's share of the sum
+
+  // `row` points at the query of this lane's column; absent ones are zeros.
+  __device__ __forceinline__ void load_query(const T* row, bool present, int lane) { x.load_query(row, present, lane); }
+  __device__ __forceinline__ void start(int lane) {
+    x.start(lane);
+#pragma unroll
+    for (int t = 0; t < S::kOut; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[t][i] = 0.0f;
+    m = -FLT_MAX;
+    l = 0.0f;
+  }
+
+  // Scores of keys outside [first, last], counted from the tile's first key, and of absent
+  // groups of 16 (bits of `absent`) become those of keys that are not seen.
+  template <int KT>
+  static __device__ __forceinline__ void mask(f32x16 (&s)[KT], int first, int last, uint32_t absent, int lane) {
+    const int h4 = 4 * (lane / 32);
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int key = 32 * kt + 8 * (i / 4) + i % 4 + h4;
+        const bool hidden = (key < first) | (key > last) | ((absent >> (2 * kt + i / 8) & 1u) != 0);
+        s[kt][i] = hidden ? -__builtin_inff() : s[kt][i];
+      }
+  }
+
+  // Weights of 32 KT keys from their scores, and the running sum.
+  template <int KT>
+  __device__ __forceinline__ void weights(const f32x16 (&s)[KT], float scale, typename P::template Weights<KT>& p) {
+    float top = s[0][0];
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) top = fmaxf(top, s[kt][i]);
+    top = max_across(top) * scale;
+    if (__builtin_amdgcn_ballot_w64(top > m + kSlack) != 0) {
+      const float to = fmaxf(m, top), by = __builtin_amdgcn_exp2f(m - to);
+      m = to;
+      l *= by;
+#pragma unroll
+      for (int t = 0; t < S::kOut; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[t][i] *= by;
+    }
+    float sum = 0.0f;
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float a = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kt][2 * i], scale, -m));
+        const float b = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kt][2 * i + 1], scale, -m));
+        sum += a + b;
+        P::set(p, kt, i, a, b);
+      }
+    l += sum;
+  }
+
+  // The product with the values key by key, adding only to the rows that see the key: a weight
+  // of zero times an infinite or NaN value of a hidden key is NaN, and the matrix cores add
+  // such products to every row of a tile.
+  template <int KT>
+  __device__ __forceinline__ void accumulate_careful(const uint8_t* values, const typename P::template Weights<KT>& p, int last, int lane) {
+#pragma unroll 1
+    for (int key = 0; key < 32 * KT; ++key) {
+      const float w = P::weight_of(p, key);
+#pragma unroll
+      for (int t = 0; t < S::kOut; ++t)
+#pragma unroll
+        for (int a = 0; a < 4; ++a) {
+          const f32x4 v = P::values_of(values, key, 32 * t + 8 * a + 4 * (lane / 32));
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[t][4 * a + e] = key <= last ? __builtin_fmaf(w, v[e], o[t][4 * a + e]) : o[t][4 * a + e];
+        }
+    }
+  }
+
+  template <int KT>
+  __device__ __forceinline__ void add(const uint8_t* values, const typename P::template Weights<KT>& p, bool careful, int last, int lane) {
+    if (careful) accumulate_careful<KT>(values, p, last, lane);
+    else x.template accumulate<KT>(values, p, o);
+  }
+
+  // 32 KT keys in LDS: rows see those of [first, last], counted from the first of them, that are
+  // in no absent group of 16; `edge` unless every row sees all of them.
+  template <int KT>
+  __device__ __forceinline__ void attend(const uint8_t* keys, const uint8_t* values, bool edge, int first, int last,
+                                         uint32_t absent, float scale, bool careful, int lane) {
+    f32x16 s[KT];
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt) x.scores(keys + 32 * kt * S::kRow, s[kt]);
+    if (edge) mask<KT>(s, first, last, absent, lane);
+    typename P::template Weights<KT> p;
+    weights<KT>(s, scale, p);
+    add<KT>(values, p, edge && careful, last, lane);
+  }
+
+  // Whether an output of this lane's row is not finite.
+  __device__ __forceinline__ bool spoiled() const {
+    float z = 0.0f;
+#pragma unroll
+    for (int t = 0; t < S::kOut; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) z = __builtin_fmaf(o[t][i], 0.0f, z);
+    return !(z == 0.0f);
+  }
+
+  // Outputs times `by` to the row at `out`.  In bf16 lane and lane ^ 32 exchange halves so that
+  // each stores 16 bytes.
+  __device__ __forceinline__ void store(T* out, bool present, float by, int lane) const {
+#pragma unroll
+    for (int t = 0; t < S::kOut; ++t) {
+      if constexpr (sizeof(T) == 2) {
+#pragma unroll
+        for (int a = 0; a < 4; a += 2) {
+          const auto x = __builtin_amdgcn_permlane32_swap(pack_bf16x2(o[t][4 * a] * by, o[t][4 * a + 1] * by),
+                                                          pack_bf16x2(o[t][4 * a + 4] * by, o[t][4 * a + 5] * by), false, false);
+          const auto y = __builtin_amdgcn_permlane32_swap(pack_bf16x2(o[t][4 * a + 2] * by, o[t][4 * a + 3] * by),
+                                                          pack_bf16x2(o[t][4 * a + 6] * by, o[t][4 * a + 7] * by), false, false);
+          if (present) *reinterpret_cast<u32x4*>(out + 32 * t + 8 * a + 8 * (lane / 32)) = u32x4{x[0], y[0], x[1], y[1]};
+        }
+      } else if (present) {
+#pragma unroll
+        for (int a = 0; a < 4; ++a)
+          *reinterpret_cast<f32x4*>(out + 32 * t + 8 * a + 4 * (lane / 32)) = f32x4{o[t][4 * a] * by, o[t][4 * a + 1] * by, o[t][4 * a + 2] * by, o[t][4 * a + 3] * by};
+      }
+    }
+  }
+};
+
+}  // namespace attention
+}  // namespace ssq

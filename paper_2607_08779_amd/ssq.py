@@ -345,3 +345,201 @@ def ssq_quantize_diag(W: torch.Tensor, group: int, q: int):
         st = getattr(lib(), fn)(_ptr(W), rows, cols, group, q, _ptr(codes), _ptr(scales), _ptr(margin), _ptr(gain))
     _check(fn, st)
     return codes, scales, margin, gain
+
+
+# --- attention (include/ssq_attention.h) ------------------------------------------------------
+
+_P, _I, _L, _F = ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_float
+_EXPORTS["ssq_page_tables"] = (_I, [_P, _P, _L, _P, _L, _P, _I, _P, _L, _L, _P, _P, _P, _P, _P, _P])
+_EXPORTS["ssq_qk_norm_rope"] = (_I, [_P, _L, _P, _L, _P, _L, _L, _I, _I, _I, _P, _P, _F, _P, _P, _L, _P, _L, _P, _L,
+                                     _P, _P, _P, _L, _I, _P])
+_EXPORTS["ssq_attention_prompt"] = (_I, [_P, _L, _P, _L, _P, _L, _P, _L, _L, _I, _I, _I, _F, _P, _L, _P])
+_EXPORTS["ssq_attention_decode"] = (_I, [_P, _L, _L, _I, _I, _I, _I, _F, _P, _P, _L, _I, _P, _L, _P, _L, _L, _P, _L, _P,
+                                         ctypes.c_size_t, _P])
+for _name in ("ssq_qk_norm_rope", "ssq_attention_prompt", "ssq_attention_decode"):
+    _EXPORTS[_name + "_f32"] = _EXPORTS[_name]
+_EXPORTS["ssq_attention_decode_workspace_size"] = (ctypes.c_size_t, [_L, _I, _I, _I, _I, _L, _L])
+
+
+def _entry(name: str, dtype: torch.dtype) -> str:
+    if dtype == torch.bfloat16:
+        return name
+    if dtype == torch.float32:
+        return name + "_f32"
+    raise TypeError("tensors must be bfloat16 or float32")
+
+
+def _heads(t: torch.Tensor, what: str, dtype: torch.dtype, tokens: Optional[int] = None) -> int:
+    """Elements between the rows of t [tokens, heads, head_dim], whose rows are contiguous."""
+    if t.dim() != 3 or t.dtype != dtype:
+        raise ValueError(f"{what} must be a [tokens, heads, head_dim] tensor of {dtype}")
+    n, heads, dim = t.shape
+    if tokens is not None and n != tokens:
+        raise ValueError(f"{what} has {n} tokens, not {tokens}")
+    stride = t.stride()
+    if stride[2] != 1 or stride[1] != dim:
+        raise ValueError(f"the heads of a token of {what} must be contiguous")
+    return stride[0] if n > 1 else heads * dim
+
+
+def _flat(t: torch.Tensor, what: str, dtype: torch.dtype, shape: Tuple[int, ...]) -> int:
+    if t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous {dtype} tensor of shape {shape}")
+    return _ptr(t)
+
+
+def ssq_page_tables(held: torch.Tensor, added: torch.Tensor, free_pages: torch.Tensor, table: torch.Tensor,
+                    page_size: int, tokens: int, taken: Optional[torch.Tensor] = None, out=None):
+    """Page table, slots and positions of a step's new tokens on the current stream.
+
+    Request r holds ``held[r]`` tokens and adds ``added[r]`` (int32); pages it needs come from
+    ``free_pages`` (int32), request after request, from entry ``taken`` (int32 [1]; None: 0) on.
+    ``table`` (int32 [requests, pages]) is updated in place.  Returns (starts [requests + 1],
+    lens [requests], positions [tokens], slots [tokens], taken after [1], table), all int32;
+    ``tokens`` may exceed the sum of ``added`` (padding: position 0, slot -1).  ``out`` = the
+    first five reuses buffers."""
+    n, i32, dev = held.shape[0] if held.dim() == 1 else -1, torch.int32, held.device
+    if table.dim() != 2 or table.shape[0] != n or table.dtype != i32 or not table.is_contiguous():
+        raise ValueError("table must be a contiguous int32 [requests, pages] tensor")
+    if out is None:
+        if tokens < 0:
+            raise ValueError("tokens must not be negative")
+        starts = torch.empty(n + 1, dtype=i32, device=dev)
+        lens = torch.empty(n, dtype=i32, device=dev)
+        positions = torch.empty(tokens, dtype=i32, device=dev)
+        slots = torch.empty(tokens, dtype=i32, device=dev)
+        after = torch.empty(1, dtype=i32, device=dev)
+    else:
+        starts, lens, positions, slots, after = out
+    st = lib().ssq_page_tables(_flat(held, "held", i32, (n,)), _flat(added, "added", i32, (n,)), n,
+                               _flat(free_pages, "free_pages", i32, (free_pages.numel(),)), free_pages.numel(),
+                               None if taken is None else _flat(taken, "taken", i32, (1,)), page_size,
+                               _ptr(table), table.shape[1], tokens, _flat(starts, "starts", i32, (n + 1,)),
+                               _flat(lens, "lens", i32, (n,)), _flat(positions, "positions", i32, (tokens,)),
+                               _flat(slots, "slots", i32, (tokens,)), _flat(after, "taken after", i32, (1,)), _stream(dev))
+    _check("ssq_page_tables", st)
+    return starts, lens, positions, slots, after, table
+
+
+def ssq_qk_norm_rope(q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor, rope: torch.Tensor,
+                     q_gain: Optional[torch.Tensor] = None, k_gain: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                     v: Optional[torch.Tensor] = None, slots: Optional[torch.Tensor] = None,
+                     k_pages: Optional[torch.Tensor] = None, v_pages: Optional[torch.Tensor] = None, out=None):
+    """Norms (where a gain is given) and position rotation of q [tokens, q_heads, head_dim] and
+    k [tokens, kv_heads, head_dim], on the current stream; returns (q, k) rotated.
+
+    bf16 (or fp32: ``ssq_qk_norm_rope_f32``); tokens may be strided, as in the rows of one fused
+    projection.  ``rope`` fp32 [rows, head_dim] holds cosines, then sines, of each position.
+    With ``slots`` (int32 [tokens], ``ssq_page_tables``) the rotated k and the given v also go to
+    the caches k_pages, v_pages [pages, kv_heads, page_size, head_dim].  ``out`` = (q, k) reuses
+    buffers (k may be None with a cache; they may be q and k themselves)."""
+    dtype = q.dtype
+    fn = _entry("ssq_qk_norm_rope", dtype)
+    qs, ks = _heads(q, "q", dtype), _heads(k, "k", dtype, q.shape[0])
+    tokens, hq, dim = q.shape
+    hk = k.shape[1]
+    if k.shape[2] != dim or rope.dim() != 2 or rope.shape[1] != dim:
+        raise ValueError("q, k and rope must have the same head_dim")
+    cache = slots is not None
+    if cache != (k_pages is not None) or cache != (v_pages is not None) or (cache and v is None):
+        raise ValueError("slots, k_pages and v_pages go together, with v")
+    vs = pages = page_size = 0
+    if cache:
+        vs = _heads(v, "v", dtype, tokens)
+        if v.shape[1:] != k.shape[1:] or k_pages.dim() != 4 or k_pages.shape[1] != hk or k_pages.shape[3] != dim:
+            raise ValueError("v must be like k, and the caches [pages, kv_heads, page_size, head_dim]")
+        pages, page_size = k_pages.shape[0], k_pages.shape[2]
+        _flat(k_pages, "k_pages", dtype, (pages, hk, page_size, dim))
+        _flat(v_pages, "v_pages", dtype, (pages, hk, page_size, dim))
+        _flat(slots, "slots", torch.int32, (tokens,))
+    if out is None:
+        q_out = torch.empty((tokens, hq, dim), dtype=dtype, device=q.device)
+        k_out = torch.empty((tokens, hk, dim), dtype=dtype, device=q.device)
+    else:
+        q_out, k_out = out
+        if q_out.shape != q.shape or (k_out is not None and k_out.shape != k.shape):
+            raise ValueError("out must be tensors like q and k")
+    qos = _heads(q_out, "q_out", dtype)
+    kos = 0 if k_out is None else _heads(k_out, "k_out", dtype)
+    gains = [None if g is None else _flat(g, "a gain", dtype, (dim,)) for g in (q_gain, k_gain)]
+    st = getattr(lib(), fn)(_ptr(q), qs, _ptr(k), ks, _ptr(v) if cache else None, vs, tokens, hq, hk, dim, *gains, eps,
+                            _flat(positions, "positions", torch.int32, (tokens,)),
+                            _flat(rope, "rope", torch.float32, tuple(rope.shape)), rope.shape[0], _ptr(q_out), qos,
+                            _ptr(k_out), kos, _ptr(slots), _ptr(k_pages), _ptr(v_pages), pages, page_size, _stream(q.device))
+    _check(fn, st)
+    return q_out, k_out
+
+
+def ssq_attention_prompt(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, starts: torch.Tensor,
+                         scale: Optional[float] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Causal attention of packed prompts on the current stream: q [tokens, q_heads, head_dim],
+    k and v [tokens, kv_heads, head_dim], bf16 or fp32, tokens may be strided.  ``starts`` (int32
+    [requests + 1]) holds the first token of each sequence and the end of the last; tokens behind
+    it give zeros.  ``scale`` defaults to 1 / sqrt(head_dim)."""
+    dtype = q.dtype
+    fn = _entry("ssq_attention_prompt", dtype)
+    qs, ks = _heads(q, "q", dtype), _heads(k, "k", dtype, q.shape[0])
+    vs = _heads(v, "v", dtype, q.shape[0])
+    tokens, hq, dim = q.shape
+    hk = k.shape[1]
+    if k.shape != v.shape or k.shape[2] != dim:
+        raise ValueError("k and v must have the same shape, and q's head_dim")
+    if starts.dim() != 1 or starts.shape[0] < 1:
+        raise ValueError("starts must hold requests + 1 values")
+    if out is None:
+        out = torch.empty((tokens, hq, dim), dtype=dtype, device=q.device)
+    elif out.shape != q.shape:
+        raise ValueError("out must be a tensor like q")
+    st = getattr(lib(), fn)(_ptr(q), qs, _ptr(k), ks, _ptr(v), vs,
+                            _flat(starts, "starts", torch.int32, tuple(starts.shape)), starts.shape[0] - 1, tokens, hq, hk,
+                            dim, dim ** -0.5 if scale is None else scale, _ptr(out), _heads(out, "out", dtype), _stream(q.device))
+    _check(fn, st)
+    return out
+
+
+def ssq_attention_decode_workspace_size(requests: int, fresh: int, q_heads: int, kv_heads: int, head_dim: int,
+                                        max_len: int, prefix: int = 0) -> int:
+    """Bytes of scratch that let ssq_attention_decode split long caches and share a prefix."""
+    return int(lib().ssq_attention_decode_workspace_size(requests, fresh, q_heads, kv_heads, head_dim, max_len, prefix))
+
+
+def ssq_attention_decode(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, table: torch.Tensor,
+                         lens: torch.Tensor, max_len: int, prefix: int = 0, scale: Optional[float] = None,
+                         out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Attention of the new tokens q [requests, fresh, q_heads, head_dim] over the paged caches
+    [pages, kv_heads, page_size, head_dim], bf16 or fp32, on the current stream.
+
+    Request r has ``lens[r]`` tokens in the cache (int32, at most ``max_len``), its ``fresh`` new
+    ones the last of them, in the pages of ``table[r]`` (int32 [requests, pages]); the first
+    ``prefix`` tokens are the same for all requests and are read from request 0's pages, once.
+    ``workspace`` (uint8, any contents, ``ssq_attention_decode_workspace_size`` bytes) is allocated
+    where it is not given; ``scale`` defaults to 1 / sqrt(head_dim)."""
+    dtype = q.dtype
+    fn = _entry("ssq_attention_decode", dtype)
+    if q.dim() != 4 or q.stride(3) != 1 or q.stride(2) != q.shape[3] or (
+            q.shape[0] > 1 and q.shape[1] > 1 and q.stride(0) != q.shape[1] * q.stride(1)):
+        raise ValueError("q must be [requests, fresh, q_heads, head_dim], its tokens equally far apart and each contiguous")
+    n, fresh, hq, dim = q.shape
+    if k_pages.dim() != 4 or k_pages.shape[3] != dim:
+        raise ValueError("the caches must be [pages, kv_heads, page_size, head_dim]")
+    pages, hk, page_size, _ = k_pages.shape
+    if table.dim() != 2:
+        raise ValueError("table must be a contiguous int32 [requests, pages] tensor")
+    width = table.shape[1]
+    if out is None:
+        out = torch.empty((n, fresh, hq, dim), dtype=dtype, device=q.device)
+    elif out.shape != q.shape or out.dtype != dtype or not out.is_contiguous():
+        raise ValueError("out must be a contiguous tensor like q")
+    if workspace is None:
+        size = lib().ssq_attention_decode_workspace_size(n, fresh, hq, hk, dim, max_len, prefix)
+        if size:
+            workspace = torch.empty(size, dtype=torch.uint8, device=q.device)
+    stride = q.stride(1) if fresh > 1 else q.stride(0) if n > 1 else hq * dim
+    st = getattr(lib(), fn)(_ptr(q), stride, n, fresh, hq, hk, dim, dim ** -0.5 if scale is None else scale,
+                            _flat(k_pages, "k_pages", dtype, (pages, hk, page_size, dim)),
+                            _flat(v_pages, "v_pages", dtype, (pages, hk, page_size, dim)), pages, page_size,
+                            _flat(table, "table", torch.int32, (n, width)), width, _flat(lens, "lens", torch.int32, (n,)), max_len,
+                            prefix, _ptr(out), hq * dim, _ptr(workspace),
+                            0 if workspace is None else workspace.numel() * workspace.element_size(), _stream(q.device))
+    _check(fn, st)
+    return out

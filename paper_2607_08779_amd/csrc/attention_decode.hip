@@ -16,6 +16,7 @@
 // Parts leave O unnormalised in binary32 with its reference and sum, and are joined as
 //   out = sum_s 2^(m_s - M) O_s / sum_s 2^(m_s - M) l_s,   M = max_s m_s.
 #include <algorithm>
+#include <type_traits>
 
 #include "attention_tiles.h"
 
@@ -126,8 +127,7 @@ __device__ __forceinline__ void put(const Decode<T>& a, const Plan& p, const Par
 }
 
 template <typename T, int D>
-__device__ void wide(const Decode<T>& a, const Plan& p, const Parts& parts, int head, int tile, int part, uint8_t* const (&lds)[4],
-                     int* spoiled) {
+__device__ void wide(const Decode<T>& a, const Plan& p, const Parts& parts, int head, int tile, int part, uint8_t* lds, int* spoiled) {
   using S = Shape<T, D>;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int prefix = (int)min(a.prefix, min(a.max_len, a.table_stride << a.cache.page_shift));
@@ -147,46 +147,46 @@ __device__ void wide(const Decode<T>& a, const Plan& p, const Parts& parts, int 
   const Loader<T, D> load(lane, S::kRow);
   const float scale = a.scale * kLog2e;
   const Pages pages = {a.table};
-  auto fill = [&](int j, uint8_t* k, uint8_t* v) {
-    const int first = j + 16 * wave, count = min(end - first, 16);
-    int64_t page = 0;
-    const bool here = count > 0 && pages.find(a.cache, first, &page);
-    const int64_t at = here ? group_offset<T, D>(a, head, page, first) : 0;
-    const uint32_t bytes = here ? (uint32_t)(count * S::kRow) : 0u;
-    load.keys(make_rsrc(a.cache.k + at, bytes), k + wave * S::kGroup);
-    load.values(make_rsrc(a.cache.v + at, bytes), v + wave * S::kGroup);
-  };
-  auto use = [&](int j, const uint8_t* k, const uint8_t* v, bool careful) {
-    if (j > wave_last) return;
-    uint32_t absent = 0;
+  auto walk = [&](auto careful) {
+    int k_at = begin + 16 * wave, v_at = k_at;            // this wavefront's 16 keys of the next tile
+    auto group = [&](const T* pool, int first) {
+      const int count = min(end - first, 16);
+      int64_t page = 0;
+      const bool here = count > 0 && pages.find(a.cache, first, &page);
+      return describe(pool + (here ? group_offset<T, D>(a, head, page, first) : 0), here ? (uint32_t)(count * S::kRow) : 0u);
+    };
+    auto absent = [&](int j) {                            // groups of 16 keys whose page is
+      uint32_t groups = 0;
 #pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      int64_t page;
-      if (j + 16 * g < end && !pages.find(a.cache, j + 16 * g, &page)) absent |= 1u << g;
-    }
-    r.template attend<2>(k, v, j + kWideKeys - 1 > wave_first || absent != 0, 0, min(row.last, end - 1) - j, absent, scale, careful, lane);
+      for (int g = 0; g < 4; ++g) {
+        int64_t page;
+        if (j + 16 * g < end && !pages.find(a.cache, j + 16 * g, &page)) groups |= 1u << g;
+      }
+      return groups;
+    };
+    walk_shared<decltype(careful)::value>(
+        r, lds, (end - begin + kWideKeys - 1) / kWideKeys, wave_last < begin ? 0 : (min(wave_last, end - 1) - begin) / kWideKeys + 1, scale, lane,
+        [&](uint8_t* to) {
+          load.keys(group(a.cache.k, k_at), to + wave * S::kGroup);
+          k_at += kWideKeys;
+        },
+        [&](uint8_t* to) {
+          load.values(group(a.cache.v, v_at), to + wave * S::kGroup);
+          v_at += kWideKeys;
+        },
+        [&](int t) { return begin + kWideKeys * (t + 1) - 1 > min(wave_first, end - 1) || absent(begin + kWideKeys * t) != 0; },
+        [&](int t, f32x16 (&s)[2]) {
+          const int j = begin + kWideKeys * t;
+          Rows32<T, D>::template mask<2>(s, 0, min(row.last, end - 1) - j, absent(j), lane);
+        },
+        [&](int t) { return min(row.last, end - 1) - begin - kWideKeys * t; });
   };
   if (threadIdx.x == 0) *spoiled = 0;
-  for (bool careful = false;; careful = true) {
-    r.start(lane);
-    if (begin < end) fill(begin, lds[0], lds[1]);
-    for (int j = begin; j < end; j += 2 * kWideKeys) {
-      wait_vmcnt<0>();
-      lds_barrier();
-      if (j + kWideKeys < end) fill(j + kWideKeys, lds[2], lds[3]);
-      use(j, lds[0], lds[1], careful);
-      if (j + kWideKeys >= end) break;
-      wait_vmcnt<0>();
-      lds_barrier();
-      if (j + 2 * kWideKeys < end) fill(j + 2 * kWideKeys, lds[0], lds[1]);
-      use(j + kWideKeys, lds[2], lds[3], careful);
-    }
-    if (careful) break;
-    __syncthreads();
-    if (row.present && r.spoiled()) *spoiled = 1;
-    __syncthreads();
-    if (*spoiled == 0) break;
-  }
+  walk(std::false_type{});
+  __syncthreads();
+  if (row.present && r.spoiled()) *spoiled = 1;
+  __syncthreads();
+  if (*spoiled != 0) walk(std::true_type{});
   const float l = sum_across(r.l);
   if (!row.present) return;
 #pragma unroll
@@ -222,7 +222,7 @@ __device__ void narrow(const Decode<T>& a, const Plan& p, const Parts& parts, in
   const Loader<T, D> load(lane, S::kRow);
   const float scale = a.scale * kLog2e;
   uint8_t *k = lds + wave * 4 * S::kGroup, *v = k + 2 * S::kGroup;
-  for (bool careful = false;; careful = true) {
+  auto walk = [&](auto careful) {
     r.start(lane);
 #pragma unroll 1
     for (int s = 0; s < 2; ++s) {
@@ -248,9 +248,9 @@ __device__ void narrow(const Decode<T>& a, const Plan& p, const Parts& parts, in
       int j = (lo & ~15) + 32 * wave;
       Group now[2] = {find(j), find(j + 16)};
 #pragma unroll
-      for (int g = 0; g < 2; ++g) load.keys(make_rsrc(a.cache.k + now[g].at, now[g].bytes), k + g * S::kGroup, lo - (j + 16 * g));
+      for (int g = 0; g < 2; ++g) load.keys(describe(a.cache.k + now[g].at, now[g].bytes), k + g * S::kGroup, lo - (j + 16 * g));
 #pragma unroll
-      for (int g = 0; g < 2; ++g) load.values(make_rsrc(a.cache.v + now[g].at, now[g].bytes), v + g * S::kGroup, lo - (j + 16 * g));
+      for (int g = 0; g < 2; ++g) load.values(describe(a.cache.v + now[g].at, now[g].bytes), v + g * S::kGroup, lo - (j + 16 * g));
       for (; j < hi; j += kNarrowKeys) {
         const int next_j = j + kNarrowKeys;
         const Group next[2] = {find(next_j), find(next_j + 16)};
@@ -258,25 +258,27 @@ __device__ void narrow(const Decode<T>& a, const Plan& p, const Parts& parts, in
         const bool edge = j + 31 > min(wave_first, hi - 1) || j < lo || absent != 0;
         landed<2 * S::kLoads>();
         f32x16 x[1];
-        r.x.scores(k, x[0]);
+        r.scores(k, x);
         have_read();
 #pragma unroll
-        for (int g = 0; g < 2; ++g) load.keys(make_rsrc(a.cache.k + next[g].at, next[g].bytes), k + g * S::kGroup, 0);
+        for (int g = 0; g < 2; ++g) load.keys(describe(a.cache.k + next[g].at, next[g].bytes), k + g * S::kGroup, 0);
         if (edge) Rows32<T, D>::template mask<1>(x, lo - j, min(row.last, hi - 1) - j, absent, lane);
         typename Products<T, D>::template Weights<1> w;
+        r.template raise<1>(x, scale);
         r.template weights<1>(x, scale, w);
         landed<2 * S::kLoads>();
-        r.template add<1>(v, w, edge && careful, min(row.last, hi - 1) - j, lane);
+        r.template add<decltype(careful)::value, 1>(v, w, edge, min(row.last, hi - 1) - j, lane);
         have_read();
 #pragma unroll
-        for (int g = 0; g < 2; ++g) load.values(make_rsrc(a.cache.v + next[g].at, next[g].bytes), v + g * S::kGroup, 0);
+        for (int g = 0; g < 2; ++g) load.values(describe(a.cache.v + next[g].at, next[g].bytes), v + g * S::kGroup, 0);
         now[0] = next[0];
         now[1] = next[1];
       }
       landed<0>();
     }
-    if (careful || __builtin_amdgcn_ballot_w64(row.present && r.spoiled()) == 0) break;
-  }
+  };
+  walk(std::false_type{});
+  if (__builtin_amdgcn_ballot_w64(row.present && r.spoiled()) != 0) walk(std::true_type{});
   // the four wavefronts' parts, through LDS, 16-byte pieces swizzled by row
   constexpr int kPieces = D / 4;
   const float l = sum_across(r.l);
@@ -323,8 +325,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void decode_kerne
   if (block < prefix_blocks) {
     const int head = block % a.kv_heads, i = block / a.kv_heads, tile = i % p.prefix_tiles, part = i / p.prefix_tiles;
     if (p.share == kShareWide) {
-      uint8_t* const stages[4] = {lds, lds + kTile, lds + 2 * kTile, lds + 3 * kTile};
-      wide<T, D>(a, p, parts, head, tile, part, stages, &spoiled);
+      wide<T, D>(a, p, parts, head, tile, part, lds, &spoiled);
     } else {
       const int per = ((prefix + p.prefix_parts - 1) / p.prefix_parts + kNarrowKeys - 1) / kNarrowKeys * kNarrowKeys;
       const Pages pages[2] = {{a.table}, {a.table}};

@@ -6,6 +6,8 @@
 // heads share every key and value that is loaded and the causal edge is one tile wide.  It
 // walks the stretch's keys 64 at a time through two stages of LDS, the next tile on its way
 // while this one is used.
+#include <type_traits>
+
 #include "attention_tiles.h"
 
 namespace ssq {
@@ -53,7 +55,7 @@ template <typename T, int D>
 __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void prompt_kernel(const Prompt<T> a, int group) {
   using S = Shape<T, D>;
   constexpr int kTile = kTileKeys * S::kRow;
-  __shared__ __align__(1024) uint8_t k0[kTile], v0[kTile], k1[kTile], v1[kTile];
+  __shared__ __align__(1024) uint8_t lds[4 * kTile];
   __shared__ int spoiled;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int head = (int)blockIdx.x % a.kv_heads;
@@ -78,48 +80,42 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void prompt_kerne
   const int64_t line = at.begin + token, column = (head * group + row - token * group) * D;
   const int last = present ? token : -1;
   const int wave_row = row0 + 32 * wave;
-  const int wave_first = wave_row / group;                                        // seen by every row
-  const int wave_last = wave_row < rows ? (min(wave_row + 32, rows) - 1) / group : -1;
-  const int keys = (min(row0 + kTileRows, rows) - 1) / group + 1;                 // that some row sees
+  const int wave_first = __builtin_amdgcn_readfirstlane(wave_row / group);                                        // seen by every row
+  const int wave_last = __builtin_amdgcn_readfirstlane(wave_row < rows ? (min(wave_row + 32, rows) - 1) / group : -1);
+  const int keys = __builtin_amdgcn_readfirstlane((min(row0 + kTileRows, rows) - 1) / group + 1);                 // that some row sees
 
   Rows32<T, D> r;
   r.load_query(a.q.p + line * a.q.stride + column, present, lane);
   const Loader<T, D> load_k(lane, (uint32_t)(sizeof(T) * a.k.stride)), load_v(lane, (uint32_t)(sizeof(T) * a.v.stride));
   const float scale = a.scale * kLog2e;
 
-  auto fill = [&](int j, uint8_t* k, uint8_t* v) {        // keys j ... j + 63, 16 of them by each wavefront
-    const int first = j + 16 * wave, count = min(keys - first, 16);
-    const int64_t from = at.begin + first;
-    const T *kp = a.k.p + from * a.k.stride + head * D, *vp = a.v.p + from * a.v.stride + head * D;
-    load_k.keys(make_rsrc(kp, count > 0 ? (uint32_t)(sizeof(T) * ((count - 1) * a.k.stride + D)) : 0u), k + wave * S::kGroup);
-    load_v.values(make_rsrc(vp, count > 0 ? (uint32_t)(sizeof(T) * ((count - 1) * a.v.stride + D)) : 0u), v + wave * S::kGroup);
-  };
-  auto tile = [&](int j, const uint8_t* k, const uint8_t* v, bool careful) {
-    if (j > wave_last) return;
-    r.template attend<2>(k, v, j + kTileKeys - 1 > wave_first, 0, last - j, 0u, scale, careful, lane);
+  auto walk = [&](auto careful) {
+    int k_at = 16 * wave, v_at = k_at;                 // this wavefront's 16 keys of the next tile
+    const T *kp = a.k.p + (at.begin + k_at) * a.k.stride + head * D, *vp = a.v.p + (at.begin + v_at) * a.v.stride + head * D;
+    auto bytes = [&](int at, int64_t stride) { return at < keys ? (uint32_t)(sizeof(T) * ((min(keys - at, 16) - 1) * (uint32_t)stride + D)) : 0u; };
+    walk_shared<decltype(careful)::value>(
+        r, lds, (keys + kTileKeys - 1) / kTileKeys, wave_last < 0 ? 0 : wave_last / kTileKeys + 1, scale, lane,
+        [&](uint8_t* to) {
+          load_k.keys(describe(kp, bytes(k_at, a.k.stride)), to + wave * S::kGroup);
+          kp += kTileKeys * a.k.stride;
+          k_at += kTileKeys;
+        },
+        [&](uint8_t* to) {
+          load_v.values(describe(vp, bytes(v_at, a.v.stride)), to + wave * S::kGroup);
+          vp += kTileKeys * a.v.stride;
+          v_at += kTileKeys;
+        },
+        [&](int t) { return kTileKeys * t + kTileKeys - 1 > wave_first; },
+        [&](int t, f32x16 (&s)[2]) { Rows32<T, D>::template mask<2>(s, 0, last - kTileKeys * t, 0u, lane); },
+        [&](int t) { return last - kTileKeys * t; });
   };
   if (threadIdx.x == 0) spoiled = 0;
-  for (bool careful = false;; careful = true) {
-    r.start(lane);
-    fill(0, k0, v0);
-    for (int j = 0; j < keys; j += 2 * kTileKeys) {
-      wait_vmcnt<0>();
-      lds_barrier();
-      if (j + kTileKeys < keys) fill(j + kTileKeys, k1, v1);
-      tile(j, k0, v0, careful);
-      if (j + kTileKeys >= keys) break;
-      wait_vmcnt<0>();
-      lds_barrier();
-      if (j + 2 * kTileKeys < keys) fill(j + 2 * kTileKeys, k0, v0);
-      tile(j + kTileKeys, k1, v1, careful);
-    }
-    // An infinite or NaN value can have reached rows of its tile that do not see it: then
-    // once more, edge tiles key by key.
-    if (careful) break;
-    if (present && r.spoiled()) spoiled = 1;
-    __syncthreads();
-    if (spoiled == 0) break;
-  }
+  walk(std::false_type{});
+  // An infinite or NaN value can have reached rows of its tile that do not see it: then once
+  // more, edge tiles key by key.
+  if (present && r.spoiled()) spoiled = 1;
+  __syncthreads();
+  if (spoiled != 0) walk(std::true_type{});
   const float l = sum_across(r.l);
   r.store(a.out.p + line * a.out.stride + column, present, l != 0.0f ? 1.0f / l : 0.0f, lane);
 }

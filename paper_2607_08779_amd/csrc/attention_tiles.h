@@ -80,6 +80,23 @@ __device__ __forceinline__ void have_read() {
   __builtin_amdgcn_sched_barrier(0);
 }
 
+// A raw buffer descriptor in four scalar registers.
+typedef u32x4 Descriptor;
+__device__ __forceinline__ Descriptor describe(const void* base, uint32_t bytes) {
+  const uint64_t p = (uint64_t)base;
+  return Descriptor{(uint32_t)p, (uint32_t)(p >> 32) & 0xffffu, bytes, (uint32_t)kBufferWord3};
+}
+// 16 bytes of each lane into LDS at `to` + 16 lane (`to` uniform), straight from memory.  Written
+// out because the compiler, which does not see which of several such loads a read of LDS
+// depends on, waits for all of them before reads that depend on none; here the wait is the
+// caller's (landed, or wait_vmcnt and a barrier), and nothing is returned in registers.  M0 is
+// nobody else's in these kernels.
+__device__ __forceinline__ void load_lds(const Descriptor& d, uint8_t* to, uint32_t offset) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+               :
+               : "s"((uint32_t)(uintptr_t)(lds_void)to), "v"(offset), "s"(d));
+}
+
 // Loads of 16 keys into LDS by one wavefront: `stride` bytes between rows, row0 the first row of
 // the group that is to be loaded (earlier ones become zeros, as do rows past the descriptor's
 // bytes; the whole offset is the lane's, so that all of it counts in that check).
@@ -97,14 +114,12 @@ struct Loader {
       v_off[i] = (uint32_t)r * stride + 16u * (uint32_t)(c ^ value_swizzle<T, D>(r));
     }
   }
-  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t r, uint8_t* to, const uint32_t (&off)[S::kLoads], int row0) const {
+  __device__ __forceinline__ void load(const Descriptor& d, uint8_t* to, const uint32_t (&off)[S::kLoads], int row0) const {
 #pragma unroll
-    for (int i = 0; i < S::kLoads; ++i)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void)(to + 1024 * i), 16,
-                                               (int)(row + i * S::kLoadRows < row0 ? kNowhere : off[i]), 0, 0, 0);
+    for (int i = 0; i < S::kLoads; ++i) load_lds(d, to + 1024 * i, row + i * S::kLoadRows < row0 ? kNowhere : off[i]);
   }
-  __device__ __forceinline__ void keys(__amdgpu_buffer_rsrc_t r, uint8_t* to, int row0 = 0) const { load(r, to, k_off, row0); }
-  __device__ __forceinline__ void values(__amdgpu_buffer_rsrc_t r, uint8_t* to, int row0 = 0) const { load(r, to, v_off, row0); }
+  __device__ __forceinline__ void keys(const Descriptor& d, uint8_t* to, int row0 = 0) const { load(d, to, k_off, row0); }
+  __device__ __forceinline__ void values(const Descriptor& d, uint8_t* to, int row0 = 0) const { load(d, to, v_off, row0); }
 };
 
 // The products of 32 query rows with tiles of 32 keys: what depends on the element type.
@@ -116,20 +131,16 @@ struct Products<uint16_t, D> {
   using S = Shape<uint16_t, D>;
   static constexpr int kSteps = D / 16;
   bf16x8 q[kSteps];
-  uint32_t k_at[kSteps], v_at[S::kOut];
+  uint32_t k_at, v_at;            // of piece 0; the other pieces' addresses differ in bits that an XOR sets
   template <int KT>
   struct Weights {
     u32x4 w[2 * KT];               // B operands of 16 keys each
   };
 
   __device__ __forceinline__ void start(int lane) {
-    const int h = lane / 32;
-#pragma unroll
-    for (int s = 0; s < kSteps; ++s) k_at[s] = (uint32_t)((lane & 31) * S::kRow + 16 * ((2 * s + h) ^ key_swizzle<uint16_t, D>(lane & 31)));
-    const int i = lane & 15;
-#pragma unroll
-    for (int t = 0; t < S::kOut; ++t)
-      v_at[t] = (uint32_t)((4 * h + i / 4) * S::kRow + 16 * ((4 * t + 2 * ((lane / 16) & 1) + (i & 3) / 2) ^ value_swizzle<uint16_t, D>(i / 4)) + 8 * (i & 1));
+    const int h = lane / 32, i = lane & 15;
+    k_at = (uint32_t)((lane & 31) * S::kRow + 16 * (h ^ key_swizzle<uint16_t, D>(lane & 31)));
+    v_at = (uint32_t)((4 * h + i / 4) * S::kRow + 16 * ((2 * ((lane / 16) & 1) + (i & 3) / 2) ^ value_swizzle<uint16_t, D>(i / 4)) + 8 * (i & 1));
   }
   __device__ __forceinline__ void load_query(const uint16_t* row, bool present, int lane) {
 #pragma unroll
@@ -139,12 +150,11 @@ struct Products<uint16_t, D> {
       q[s] = __builtin_bit_cast(bf16x8, d);
     }
   }
-  __device__ __forceinline__ void scores(const uint8_t* keys, f32x16& s) const {
-#pragma unroll
-    for (int i = 0; i < 16; ++i) s[i] = 0.0f;
-#pragma unroll
-    for (int k = 0; k < kSteps; ++k)
-      s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(keys + k_at[k]), q[k], s, 0, 0, 0);
+  static constexpr int kPieces = kSteps;
+  typedef bf16x8 Piece;            // of 32 keys, as an A operand
+  __device__ __forceinline__ Piece key(const uint8_t* keys, int k) const { return *reinterpret_cast<const bf16x8*>(keys + (k_at ^ (uint32_t)(32 * k))); }
+  __device__ __forceinline__ void score(const Piece& key, int k, f32x16& s) const {
+    s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(key, q[k], s, 0, 0, 0);
   }
   // Weights w[2 i], w[2 i + 1] of a lane's half of tile kt, rounded to bf16.
   template <int KT>
@@ -156,7 +166,7 @@ struct Products<uint16_t, D> {
     s16x4 d[2];
 #pragma unroll
     for (int s = 0; s < 2; ++s)
-      d[s] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(values + v_at[t] + (16 * c + 8 * s) * S::kRow));
+      d[s] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(values + (v_at ^ (uint32_t)(64 * t)) + (16 * c + 8 * s) * S::kRow));
     const auto lo = __builtin_bit_cast(u32x2, d[0]), hi = __builtin_bit_cast(u32x2, d[1]);
     return __builtin_bit_cast(bf16x8, u32x4{lo.x, lo.y, hi.x, hi.y});
   }
@@ -213,15 +223,12 @@ struct Products<float, D> {
       for (int e = 0; e < 4; ++e) q[4 * u + e] = d[e];
     }
   }
-  __device__ __forceinline__ void scores(const uint8_t* keys, f32x16& s) const {
+  static constexpr int kPieces = D / 8;
+  typedef f32x4 Piece;
+  __device__ __forceinline__ Piece key(const uint8_t* keys, int u) const { return *reinterpret_cast<const f32x4*>(keys + k_base + 16 * ((2 * u) ^ k_swz)); }
+  __device__ __forceinline__ void score(const Piece& key, int u, f32x16& s) const {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) s[i] = 0.0f;
-#pragma unroll
-    for (int u = 0; u < D / 8; ++u) {
-      const f32x4 d = *reinterpret_cast<const f32x4*>(keys + k_base + 16 * ((2 * u) ^ k_swz));
-#pragma unroll
-      for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_32x32x2f32(d[e], q[4 * u + e], s, 0, 0, 0);
-    }
+    for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_32x32x2f32(key[e], q[4 * u + e], s, 0, 0, 0);
   }
   template <int KT>
   static __device__ __forceinline__ void set(Weights<KT>& p, int kt, int i, float a, float b) {
@@ -274,6 +281,28 @@ struct Rows32 {
     l = 0.0f;
   }
 
+  // S^T of 32 KT keys: the tiles in turn, each piece of the keys read four products ahead.
+  template <int KT>
+  __device__ __forceinline__ void scores(const uint8_t* keys, f32x16 (&s)[KT]) const {
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[kt][i] = 0.0f;
+#pragma unroll
+    for (int k = 0; k < P::kPieces; ++k)
+#pragma unroll
+      for (int kt = 0; kt < KT; ++kt) x.score(x.key(keys + 32 * kt * S::kRow, k), k, s[kt]);
+    if constexpr (sizeof(T) == 2) {
+      __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+      for (int i = 0; i < P::kPieces * KT - 4; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      }
+      __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
+    }
+  }
+
   // Scores of keys outside [first, last], counted from the tile's first key, and of absent
   // groups of 16 (bits of `absent`) become those of keys that are not seen.
   template <int KT>
@@ -289,16 +318,17 @@ struct Rows32 {
       }
   }
 
-  // Weights of 32 KT keys from their scores, and the running sum.
+  // Moves the reference where a score of these exceeds it by more than kSlack.  A NaN score leaves
+  // it as it is and spoils its row by its weight.
   template <int KT>
-  __device__ __forceinline__ void weights(const f32x16 (&s)[KT], float scale, typename P::template Weights<KT>& p) {
+  __device__ __forceinline__ void raise(const f32x16 (&s)[KT], float scale) {
     float top = s[0][0];
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) top = fmaxf(top, s[kt][i]);
+      for (int i = 0; i < 16; ++i) top = __builtin_elementwise_maximum(top, s[kt][i]);
     top = max_across(top) * scale;
-    if (__builtin_amdgcn_ballot_w64(top > m + kSlack) != 0) {
+    if (__builtin_expect(__builtin_amdgcn_ballot_w64(top > m + kSlack) != 0, 0)) {
       const float to = fmaxf(m, top), by = __builtin_amdgcn_exp2f(m - to);
       m = to;
       l *= by;
@@ -307,6 +337,11 @@ struct Rows32 {
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[t][i] *= by;
     }
+  }
+
+  // Weights of 32 KT keys from their scores, and the running sum.
+  template <int KT>
+  __device__ __forceinline__ void weights(const f32x16 (&s)[KT], float scale, typename P::template Weights<KT>& p) {
     float sum = 0.0f;
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt)
@@ -339,24 +374,12 @@ struct Rows32 {
     }
   }
 
-  template <int KT>
-  __device__ __forceinline__ void add(const uint8_t* values, const typename P::template Weights<KT>& p, bool careful, int last, int lane) {
-    if (careful) accumulate_careful<KT>(values, p, last, lane);
-    else x.template accumulate<KT>(values, p, o);
-  }
-
-  // 32 KT keys in LDS: rows see those of [first, last], counted from the first of them, that are
-  // in no absent group of 16; `edge` unless every row sees all of them.
-  template <int KT>
-  __device__ __forceinline__ void attend(const uint8_t* keys, const uint8_t* values, bool edge, int first, int last,
-                                         uint32_t absent, float scale, bool careful, int lane) {
-    f32x16 s[KT];
-#pragma unroll
-    for (int kt = 0; kt < KT; ++kt) x.scores(keys + 32 * kt * S::kRow, s[kt]);
-    if (edge) mask<KT>(s, first, last, absent, lane);
-    typename P::template Weights<KT> p;
-    weights<KT>(s, scale, p);
-    add<KT>(values, p, edge && careful, last, lane);
+  template <bool CAREFUL, int KT>
+  __device__ __forceinline__ void add(const uint8_t* values, const typename P::template Weights<KT>& p, bool edge, int last, int lane) {
+    if constexpr (CAREFUL) {
+      if (edge) return accumulate_careful<KT>(values, p, last, lane);
+    }
+    x.template accumulate<KT>(values, p, o);
   }
 
   // Whether an output of this lane's row is not finite.
@@ -391,6 +414,45 @@ struct Rows32 {
     }
   }
 };
+
+// Four wavefronts of 32 rows each against the same keys, which come 64 at a time through two
+// stages of LDS, the next 64 on their way while these are used.  `keys(buffer)` and
+// `values(buffer)` load this wavefront's quarter of the next 64, in order; `tiles` are walked by
+// all, the first `mine` of them matter to this wavefront's rows; `edge(t)` says whether some row
+// does not see all keys of tile t, `hide(t, s)` then masks its scores, and `last(t)` is the last
+// key of tile t that the lane's row sees.
+template <bool CAREFUL, typename T, int D, typename Keys, typename Values, typename Edge, typename Hide, typename Last>
+__device__ __forceinline__ void walk_shared(Rows32<T, D>& r, uint8_t* lds, int tiles, int mine, float scale, int lane, Keys keys,
+                                            Values values, Edge edge, Hide hide, Last last) {
+  using S = Shape<T, D>;
+  constexpr int kTile = 64 * S::kRow;
+  r.start(lane);
+  auto step = [&](int t, uint8_t* now, uint8_t* next) {
+    wait_vmcnt<0>();
+    lds_barrier();
+    if (t + 1 < tiles) {
+      keys(next);
+      values(next + kTile);
+    }
+    if (t >= mine) return;
+    f32x16 s[2];
+    r.scores(now, s);
+    const bool hidden = edge(t);
+    if (__builtin_expect(hidden, 0)) hide(t, s);
+    r.template raise<2>(s, scale);
+    typename Products<T, D>::template Weights<2> p;
+    r.template weights<2>(s, scale, p);
+    r.template add<CAREFUL, 2>(now + kTile, p, CAREFUL && hidden, CAREFUL ? last(t) : 0, lane);
+  };
+  if (tiles > 0) {
+    keys(lds);
+    values(lds + kTile);
+  }
+  for (int t = 0; t < tiles; t += 2) {
+    step(t, lds, lds + 2 * kTile);
+    if (t + 1 < tiles) step(t + 1, lds + 2 * kTile, lds);
+  }
+}
 
 }  // namespace attention
 }  // namespace ssq

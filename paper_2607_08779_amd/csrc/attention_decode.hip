@@ -62,7 +62,7 @@ Plan make_plan(int64_t requests, int fresh, int q_heads, int kv_heads, int64_t m
   if (requests > 1 && prefix > 0) {
     p.share = p.rows > kNarrowRows ? kShareWide : kShareNarrow;
     p.prefix_tiles = p.share == kShareWide ? (int)ceil_div(p.rows, kWideRows) : 1;
-    p.prefix_parts = (int)std::clamp(ceil_div(kGroups, (int64_t)p.prefix_tiles * kv_heads), (int64_t)1,
+    p.prefix_parts = (int)std::clamp(ceil_div(kGroups / 2, (int64_t)p.prefix_tiles * kv_heads), (int64_t)1,
                                      std::min<int64_t>(kMaxParts / 2, ceil_div(prefix, 256)));
   } else {
     prefix = 0;
@@ -148,37 +148,29 @@ __device__ void wide(const Decode<T>& a, const Plan& p, const Parts& parts, int 
   const float scale = a.scale * kLog2e;
   const Pages pages = {a.table};
   auto walk = [&](auto careful) {
-    int k_at = begin + 16 * wave, v_at = k_at;            // this wavefront's 16 keys of the next tile
-    auto group = [&](const T* pool, int first) {
-      const int count = min(end - first, 16);
-      int64_t page = 0;
-      const bool here = count > 0 && pages.find(a.cache, first, &page);
-      return describe(pool + (here ? group_offset<T, D>(a, head, page, first) : 0), here ? (uint32_t)(count * S::kRow) : 0u);
-    };
-    auto absent = [&](int j) {                            // groups of 16 keys whose page is
-      uint32_t groups = 0;
-#pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        int64_t page;
-        if (j + 16 * g < end && !pages.find(a.cache, j + 16 * g, &page)) groups |= 1u << g;
-      }
-      return groups;
-    };
+    uint32_t absent = 0, next_absent = 0;                 // groups of 16 keys of this tile and the next whose page is
+    int64_t at = 0;                                       // this wavefront's group of the next tile
+    uint32_t bytes = 0;
     walk_shared<decltype(careful)::value>(
         r, lds, (end - begin + kWideKeys - 1) / kWideKeys, wave_last < begin ? 0 : (min(wave_last, end - 1) - begin) / kWideKeys + 1, scale, lane,
-        [&](uint8_t* to) {
-          load.keys(group(a.cache.k, k_at), to + wave * S::kGroup);
-          k_at += kWideKeys;
+        [&](int t) {
+          const int j = begin + kWideKeys * t, first = j + 16 * wave;
+          absent = next_absent;
+          next_absent = 0;
+          bytes = 0;
+          int64_t page;
+          if (first < end && pages.find(a.cache, first, &page)) {
+            at = group_offset<T, D>(a, head, page, first);
+            bytes = (uint32_t)(min(end - first, 16) * S::kRow);
+          }
+#pragma unroll
+          for (int g = 0; g < 4; ++g)
+            if (j + 16 * g < end && !pages.find(a.cache, j + 16 * g, &page)) next_absent |= 1u << g;
         },
-        [&](uint8_t* to) {
-          load.values(group(a.cache.v, v_at), to + wave * S::kGroup);
-          v_at += kWideKeys;
-        },
-        [&](int t) { return begin + kWideKeys * (t + 1) - 1 > min(wave_first, end - 1) || absent(begin + kWideKeys * t) != 0; },
-        [&](int t, f32x16 (&s)[2]) {
-          const int j = begin + kWideKeys * t;
-          Rows32<T, D>::template mask<2>(s, 0, min(row.last, end - 1) - j, absent(j), lane);
-        },
+        [&](uint8_t* to) { load.keys(describe(a.cache.k + at, bytes), to + wave * S::kGroup); },
+        [&](uint8_t* to) { load.values(describe(a.cache.v + at, bytes), to + wave * S::kGroup); },
+        [&](int t) { return begin + kWideKeys * (t + 1) - 1 > min(wave_first, end - 1) || absent != 0; },
+        [&](int t, f32x16 (&s)[2]) { Rows32<T, D>::template mask<2>(s, 0, min(row.last, end - 1) - begin - kWideKeys * t, absent, lane); },
         [&](int t) { return min(row.last, end - 1) - begin - kWideKeys * t; });
   };
   if (threadIdx.x == 0) *spoiled = 0;
@@ -196,11 +188,16 @@ __device__ void wide(const Decode<T>& a, const Plan& p, const Parts& parts, int 
       put<T, D>(a, p, parts, part, row, 32 * t + 8 * i + 4 * (lane / 32), f32x4{r.o[t][4 * i], r.o[t][4 * i + 1], r.o[t][4 * i + 2], r.o[t][4 * i + 3]}, r.m, l);
 }
 
-// Rows `tile0` ... of `request` (of all requests if it is negative) against keys
-// [begin[s], end[s]) of the table rows `pages[s]`.
+// Keys [begin, end) of a table row.
+struct Range {
+  const int32_t* row;
+  int begin, end;
+};
+
+// Rows from `index0` on of `request` (of all requests if it is negative) against two ranges.
 template <typename T, int D>
 __device__ void narrow(const Decode<T>& a, const Plan& p, const Parts& parts, int head, int request, int index0,
-                       const Pages (&pages)[2], const int (&begin)[2], const int (&end)[2], int part, uint8_t* lds, float2* ml) {
+                       const Range (&range)[2], int part, uint8_t* lds, float2* ml) {
   using S = Shape<T, D>;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int rows = request < 0 ? p.rows : a.fresh * p.group;
@@ -226,8 +223,8 @@ __device__ void narrow(const Decode<T>& a, const Plan& p, const Parts& parts, in
     r.start(lane);
 #pragma unroll 1
     for (int s = 0; s < 2; ++s) {
-      const int lo = s == 0 ? begin[0] : begin[1], hi = s == 0 ? end[0] : end[1];
-      const Pages of = {s == 0 ? pages[0].row : pages[1].row};
+      const int lo = s == 0 ? range[0].begin : range[1].begin, hi = s == 0 ? range[0].end : range[1].end;
+      const Pages of = {s == 0 ? range[0].row : range[1].row};
       if (lo >= hi) continue;
       struct Group {
         int64_t at;
@@ -315,70 +312,90 @@ __device__ void narrow(const Decode<T>& a, const Plan& p, const Parts& parts, in
 }
 
 template <typename T, int D>
-__global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void decode_kernel(const Decode<T> a, const Plan p, const Parts parts, int prefix_blocks) {
+__global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void decode_kernel(const Decode<T> a, const Plan p, const Parts parts, int prefix_groups, int own_groups) {
   constexpr int kTile = 64 * Shape<T, D>::kRow;
   __shared__ __align__(1024) uint8_t lds[4 * kTile];
   __shared__ float2 ml[kWaves * 32];
   __shared__ int spoiled;
-  const int block = (int)blockIdx.x;
   const int prefix = (int)min(a.prefix, min(a.max_len, a.table_stride << a.cache.page_shift));
-  if (block < prefix_blocks) {
-    const int head = block % a.kv_heads, i = block / a.kv_heads, tile = i % p.prefix_tiles, part = i / p.prefix_tiles;
-    if (p.share == kShareWide) {
-      wide<T, D>(a, p, parts, head, tile, part, lds, &spoiled);
-    } else {
-      const int per = ((prefix + p.prefix_parts - 1) / p.prefix_parts + kNarrowKeys - 1) / kNarrowKeys * kNarrowKeys;
-      const Pages pages[2] = {{a.table}, {a.table}};
-      const int begin[2] = {min(part * per, prefix), 0}, end[2] = {min((part + 1) * per, prefix), 0};
-      narrow<T, D>(a, p, parts, head, -1, 0, pages, begin, end, part, lds, ml);
-    }
+  // the heads in turn; of the rest, work on the prefix (arithmetic) and on the requests' own keys
+  // (memory) in turn while there are both, so that a CU has some of each
+  const int head = (int)blockIdx.x % a.kv_heads, turn = (int)blockIdx.x / a.kv_heads;
+  const int both = 2 * min(prefix_groups, own_groups);
+  const bool on_prefix = turn < both ? turn % 2 == 0 : prefix_groups > own_groups;
+  const int i0 = turn < both ? turn / 2 : turn - both / 2;
+  // what lies in the prefix comes from the first request's pages, shared or not
+  Range range[2] = {{a.table, 0, 0}, {a.table, 0, 0}};
+  int request = -1, index0 = 0, part;
+  if (on_prefix) {
+    const int tile = i0 % p.prefix_tiles;
+    part = i0 / p.prefix_tiles;
+    if (p.share == kShareWide) return wide<T, D>(a, p, parts, head, tile, part, lds, &spoiled);
+    const int per = ((prefix + p.prefix_parts - 1) / p.prefix_parts + kNarrowKeys - 1) / kNarrowKeys * kNarrowKeys;
+    range[0].begin = min(part * per, prefix);
+    range[0].end = min(range[0].begin + per, prefix);
   } else {
-    const int i0 = block - prefix_blocks, head = i0 % a.kv_heads;
-    int i = i0 / a.kv_heads;
-    const int part = i % p.own_parts;
+    int i = i0;
+    part = i % p.own_parts;
     i /= p.own_parts;
-    const int tile = i % p.own_tiles, request = i / p.own_tiles;
+    index0 = i % p.own_tiles * kNarrowRows;
+    request = i / p.own_tiles;
     const int len = request_len(a, request), from = min(p.share != kShareNone ? prefix : 0, len);
     const int per = ((len - from + p.own_parts - 1) / p.own_parts + kNarrowKeys - 1) / kNarrowKeys * kNarrowKeys;
     const int lo = min(from + part * per, len), hi = min(lo + per, len);
-    // what lies in the prefix comes from the first request's pages, shared or not
-    const Pages pages[2] = {{a.table}, {a.table + request * a.table_stride}};
-    const int begin[2] = {lo, max(lo, prefix)}, end[2] = {min(hi, prefix), hi};
-    narrow<T, D>(a, p, parts, head, request, tile * kNarrowRows, pages, begin, end, p.share != kShareNone ? p.prefix_parts + part : part, lds, ml);
+    range[0].begin = lo;
+    range[0].end = min(hi, prefix);
+    range[1] = {a.table + request * a.table_stride, max(lo, prefix), hi};
+    if (p.share != kShareNone) part += p.prefix_parts;
   }
+  narrow<T, D>(a, p, parts, head, request, index0, range, part, lds, ml);
 }
 
-// One row of out from its parts, a wavefront each.
+// One row of out from its parts, by a workgroup: D / 4 lanes hold the row, and the groups of so
+// many lanes take the parts in turn, so that all their loads are under way at once.
 template <typename T, int D>
 __global__ __launch_bounds__(kThreads) void join_kernel(const Decode<T> a, int64_t line_rows, int count, const Parts parts) {
-  constexpr int E = D / 64;
-  const int lane = threadIdx.x & 63;
-  const int64_t row = (int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6);
-  if (row >= line_rows) return;
+  constexpr int kLanes = D / 4, kGroups = kThreads / kLanes;
+  __shared__ f32x4 sums[kGroups][kLanes];
+  const int lane = threadIdx.x & 63, at = (int)threadIdx.x % kLanes, group = (int)threadIdx.x / kLanes;
+  const int64_t row = blockIdx.x;
+  const float* from = parts.o + row * D + 4 * at;
+  constexpr int kAhead = 4;
+  f32x4 o[kAhead];
+#pragma unroll
+  for (int i = 0; i < kAhead; ++i) {
+    const int s = group + i * kGroups;
+    o[i] = s < count ? *reinterpret_cast<const f32x4*>(from + s * line_rows * D) : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  }
+  // every wavefront forms the parts' weights, for itself
   const float2 x = lane < count ? parts.ml[lane * line_rows + row] : float2{-FLT_MAX, 0.0f};
   float m = x.y != 0.0f ? x.x : -FLT_MAX;
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+  for (int d = 32; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor(m, d, 64));
   const float by = x.y != 0.0f ? __builtin_amdgcn_exp2f(x.x - m) : 0.0f;
   float l = by * x.y;
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) l += __shfl_xor(l, o, 64);
-  float sum[E] = {};
-  for (int s = 0; s < count; ++s) {
-    const float w = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(by), s));
-    if (__uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x.y), s)) == 0.0f) continue;
-    const float* o = parts.o + (s * line_rows + row) * D + E * lane;
+  for (int d = 32; d > 0; d >>= 1) l += __shfl_xor(l, d, 64);
+  f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-    for (int e = 0; e < E; ++e) sum[e] = __builtin_fmaf(w, o[e], sum[e]);
+  for (int i = 0; i < kMaxParts / kGroups; ++i) {
+    const int s = group + i * kGroups;
+    if (i * kGroups >= count) break;
+    const float w = __shfl(by, s, 64);
+    const f32x4 y = i < kAhead ? o[i] : s < count ? *reinterpret_cast<const f32x4*>(from + s * line_rows * D) : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sum[e] = __builtin_fmaf(w, y[e], sum[e]);
   }
-  const float inv = l != 0.0f ? 1.0f / l : 0.0f;
+  sums[group][at] = sum;
+  __syncthreads();
+  if (group != 0) return;
+#pragma unroll
+  for (int g = 1; g < kGroups; ++g)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sum[e] += sums[g][at][e];
   const int64_t line = row / a.q_heads;
-  T* out = a.out.p + line * a.out.stride + (row - line * a.q_heads) * D + E * lane;
-#pragma unroll
-  for (int e = 0; e < E; ++e) {
-    if constexpr (sizeof(T) == 2) out[e] = f32_to_bf16_bits(sum[e] * inv);
-    else out[e] = sum[e] * inv;
-  }
+  const Row to = {true, line, (int)(row - line * a.q_heads), 0};
+  put<T, D>(a, Plan{}, Parts{nullptr, nullptr}, 0, to, 4 * at, sum, 0.0f, l);
 }
 
 size_t part_bytes(const Plan& p, int head_dim) {
@@ -398,10 +415,9 @@ hipError_t launch(const Decode<T>& a, void* workspace, size_t workspace_bytes, h
     parts.o = static_cast<float*>(workspace);
     parts.ml = reinterpret_cast<float2*>(parts.o + (size_t)p.parts() * p.line_rows * D);
   }
-  const int64_t prefix_blocks = p.prefix_groups() * a.kv_heads;
-  const int64_t blocks = prefix_blocks + a.requests * p.own_tiles * p.own_parts * a.kv_heads;
-  decode_kernel<T, D><<<dim3((unsigned)blocks), kThreads, 0, stream>>>(a, p, parts, (int)prefix_blocks);
-  if (need > 0) join_kernel<T, D><<<dim3((unsigned)ceil_div(p.line_rows, kWaves)), kThreads, 0, stream>>>(a, p.line_rows, p.parts(), parts);
+  const int64_t prefix_groups = p.prefix_groups(), own_groups = a.requests * p.own_tiles * p.own_parts;
+  decode_kernel<T, D><<<dim3((unsigned)((prefix_groups + own_groups) * a.kv_heads)), kThreads, 0, stream>>>(a, p, parts, (int)prefix_groups, (int)own_groups);
+  if (need > 0) join_kernel<T, D><<<dim3((unsigned)p.line_rows), kThreads, 0, stream>>>(a, p.line_rows, p.parts(), parts);
   return hipGetLastError();
 }
 

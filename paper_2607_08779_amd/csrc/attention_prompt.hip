@@ -94,7 +94,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void prompt_kerne
     const T *kp = a.k.p + (at.begin + k_at) * a.k.stride + head * D, *vp = a.v.p + (at.begin + v_at) * a.v.stride + head * D;
     auto bytes = [&](int at, int64_t stride) { return at < keys ? (uint32_t)(sizeof(T) * ((min(keys - at, 16) - 1) * (uint32_t)stride + D)) : 0u; };
     walk_shared<decltype(careful)::value>(
-        r, lds, (keys + kTileKeys - 1) / kTileKeys, wave_last < 0 ? 0 : wave_last / kTileKeys + 1, scale, lane,
+        r, lds, (keys + kTileKeys - 1) / kTileKeys, wave_last < 0 ? 0 : wave_last / kTileKeys + 1, scale, lane, [](int) {},
         [&](uint8_t* to) {
           load_k.keys(describe(kp, bytes(k_at, a.k.stride)), to + wave * S::kGroup);
           kp += kTileKeys * a.k.stride;

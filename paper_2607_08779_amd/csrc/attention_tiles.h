@@ -416,25 +416,29 @@ struct Rows32 {
 };
 
 // Four wavefronts of 32 rows each against the same keys, which come 64 at a time through two
-// stages of LDS, the next 64 on their way while these are used.  `keys(buffer)` and
+// stages of LDS, the next 64 on their way while these are used.  `ahead(t)` looks up what the
+// loads of tile t need, before the wait for those of tile t - 1, `keys(buffer)` and
 // `values(buffer)` load this wavefront's quarter of the next 64, in order; `tiles` are walked by
 // all, the first `mine` of them matter to this wavefront's rows; `edge(t)` says whether some row
 // does not see all keys of tile t, `hide(t, s)` then masks its scores, and `last(t)` is the last
 // key of tile t that the lane's row sees.
-template <bool CAREFUL, typename T, int D, typename Keys, typename Values, typename Edge, typename Hide, typename Last>
-__device__ __forceinline__ void walk_shared(Rows32<T, D>& r, uint8_t* lds, int tiles, int mine, float scale, int lane, Keys keys,
-                                            Values values, Edge edge, Hide hide, Last last) {
+template <bool CAREFUL, typename T, int D, typename Ahead, typename Keys, typename Values, typename Edge, typename Hide, typename Last>
+__device__ __forceinline__ void walk_shared(Rows32<T, D>& r, uint8_t* lds, int tiles, int mine, float scale, int lane, Ahead ahead,
+                                            Keys keys, Values values, Edge edge, Hide hide, Last last) {
   using S = Shape<T, D>;
   constexpr int kTile = 64 * S::kRow;
   r.start(lane);
-  auto step = [&](int t, uint8_t* now, uint8_t* next) {
+  auto turn = [&](int t, uint8_t* next) {              // tile t is there, t + 1 on its way
+    ahead(t + 1);
     wait_vmcnt<0>();
     lds_barrier();
     if (t + 1 < tiles) {
       keys(next);
       values(next + kTile);
     }
-    if (t >= mine) return;
+  };
+  auto step = [&](int t, uint8_t* now, uint8_t* next) {
+    turn(t, next);
     f32x16 s[2];
     r.scores(now, s);
     const bool hidden = edge(t);
@@ -444,14 +448,17 @@ __device__ __forceinline__ void walk_shared(Rows32<T, D>& r, uint8_t* lds, int t
     r.template weights<2>(s, scale, p);
     r.template add<CAREFUL, 2>(now + kTile, p, CAREFUL && hidden, CAREFUL ? last(t) : 0, lane);
   };
+  uint8_t *const a = lds, *const b = lds + 2 * kTile;
   if (tiles > 0) {
-    keys(lds);
-    values(lds + kTile);
+    ahead(0);
+    keys(a);
+    values(a + kTile);
   }
-  for (int t = 0; t < tiles; t += 2) {
-    step(t, lds, lds + 2 * kTile);
-    if (t + 1 < tiles) step(t + 1, lds + 2 * kTile, lds);
+  for (int t = 0; t < mine; t += 2) {
+    step(t, a, b);
+    if (t + 1 < mine) step(t + 1, b, a);
   }
+  for (int t = mine; t < tiles; ++t) turn(t, t & 1 ? a : b);       // the others' tiles
 }
 
 }  // namespace attention

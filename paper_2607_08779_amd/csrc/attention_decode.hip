@@ -218,97 +218,33 @@ __device__ void narrow(const Decode<T>& a, const Plan& p, const Parts& parts, in
   r.load_query(a.q.p + row.line * a.q.stride + row.column * D, row.present, lane);
   const Loader<T, D> load(lane, S::kRow);
   const float scale = a.scale * kLog2e;
-  uint8_t *k = lds + wave * 4 * S::kGroup, *v = k + 2 * S::kGroup;
   auto walk = [&](auto careful) {
     r.start(lane);
 #pragma unroll 1
     for (int s = 0; s < 2; ++s) {
       const int lo = s == 0 ? range[0].begin : range[1].begin, hi = s == 0 ? range[0].end : range[1].end;
       const Pages of = {s == 0 ? range[0].row : range[1].row};
-      if (lo >= hi) continue;
-      struct Group {
-        int64_t at;
-        uint32_t bytes;
-        bool absent;
-      };
-      auto find = [&](int first) {                       // 16 keys from a multiple of 16 on
-        Group g = {0, 0u, false};
+      walk_private<decltype(careful)::value>(r, lds, load, load, wave, kWaves, lo, hi, wave_first, row.last, scale, lane, [&](int first) {
+        Group<T> g = {a.cache.k, a.cache.v, 0u, 0u, false};
         const int count = min(hi - first, 16);
         if (count > 0) {
           int64_t page;
-          const bool here = of.find(a.cache, first, &page);
-          g.absent = !here;
-          if (here) g.at = group_offset<T, D>(a, head, page, first), g.bytes = (uint32_t)(count * S::kRow);
+          g.absent = !of.find(a.cache, first, &page);
+          if (!g.absent) {
+            const int64_t at = group_offset<T, D>(a, head, page, first);
+            g.k += at;
+            g.v += at;
+            g.k_bytes = g.v_bytes = (uint32_t)(count * S::kRow);
+          }
         }
         return g;
-      };
-      int j = (lo & ~15) + 32 * wave;
-      Group now[2] = {find(j), find(j + 16)};
-#pragma unroll
-      for (int g = 0; g < 2; ++g) load.keys(describe(a.cache.k + now[g].at, now[g].bytes), k + g * S::kGroup, lo - (j + 16 * g));
-#pragma unroll
-      for (int g = 0; g < 2; ++g) load.values(describe(a.cache.v + now[g].at, now[g].bytes), v + g * S::kGroup, lo - (j + 16 * g));
-      for (; j < hi; j += kNarrowKeys) {
-        const int next_j = j + kNarrowKeys;
-        const Group next[2] = {find(next_j), find(next_j + 16)};
-        const uint32_t absent = (now[0].absent ? 1u : 0u) | (now[1].absent ? 2u : 0u);
-        const bool edge = j + 31 > min(wave_first, hi - 1) || j < lo || absent != 0;
-        landed<2 * S::kLoads>();
-        f32x16 x[1];
-        r.scores(k, x);
-        have_read();
-#pragma unroll
-        for (int g = 0; g < 2; ++g) load.keys(describe(a.cache.k + next[g].at, next[g].bytes), k + g * S::kGroup, 0);
-        if (edge) Rows32<T, D>::template mask<1>(x, lo - j, min(row.last, hi - 1) - j, absent, lane);
-        typename Products<T, D>::template Weights<1> w;
-        r.template raise<1>(x, scale);
-        r.template weights<1>(x, scale, w);
-        landed<2 * S::kLoads>();
-        r.template add<decltype(careful)::value, 1>(v, w, edge, min(row.last, hi - 1) - j, lane);
-        have_read();
-#pragma unroll
-        for (int g = 0; g < 2; ++g) load.values(describe(a.cache.v + next[g].at, next[g].bytes), v + g * S::kGroup, 0);
-        now[0] = next[0];
-        now[1] = next[1];
-      }
-      landed<0>();
+      });
     }
   };
   walk(std::false_type{});
   if (__builtin_amdgcn_ballot_w64(row.present && r.spoiled()) != 0) walk(std::true_type{});
-  // the four wavefronts' parts, through LDS, 16-byte pieces swizzled by row
-  constexpr int kPieces = D / 4;
-  const float l = sum_across(r.l);
-  __syncthreads();
-  f32x4* const o = reinterpret_cast<f32x4*>(lds);
-  const int n = lane & 31, count = min(rows - index0, kNarrowRows);
-  if (n < count) {
-#pragma unroll
-    for (int t = 0; t < S::kOut; ++t)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        o[(wave * 32 + n) * kPieces + ((8 * t + 2 * i + lane / 32) ^ (n % kPieces))] = f32x4{r.o[t][4 * i], r.o[t][4 * i + 1], r.o[t][4 * i + 2], r.o[t][4 * i + 3]};
-    if (lane < 32) ml[wave * 32 + n] = float2{r.m, l};
-  }
-  __syncthreads();
-  for (int i = threadIdx.x; i < count * kPieces; i += kThreads) {
-    const int at = i % kPieces, of = i / kPieces;
-    float m = ml[of].x, sum = 0.0f;
-#pragma unroll
-    for (int w = 1; w < kWaves; ++w) m = fmaxf(m, ml[w * 32 + of].x);
-    f32x4 all = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-      const float2 x = ml[w * 32 + of];
-      if (x.y == 0.0f) continue;
-      const float by = __builtin_amdgcn_exp2f(x.x - m);
-      const f32x4 y = o[(w * 32 + of) * kPieces + (at ^ (of % kPieces))];
-      sum = __builtin_fmaf(by, x.y, sum);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) all[e] = __builtin_fmaf(by, y[e], all[e]);
-    }
-    put<T, D>(a, p, parts, part, find_row(of), 4 * at, all, m, sum);
-  }
+  join_waves<kWaves>(r, lds, ml, min(rows - index0, kNarrowRows), wave, lane,
+                     [&](int of, int at, f32x4 o, float m, float l) { put<T, D>(a, p, parts, part, find_row(of), at, o, m, l); });
 }
 
 template <typename T, int D>

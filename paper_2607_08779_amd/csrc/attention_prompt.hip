@@ -21,6 +21,7 @@ constexpr int kWaves = 4, kThreads = 64 * kWaves, kTileRows = 32 * kWaves, kTile
 struct Place {
   int begin, end, tile, tiles;
 };
+template <int ROWS>
 __device__ __forceinline__ bool find_tile(const int32_t* starts, int requests, int tokens, int group, int* rank, Place* at) {
   const int lane = threadIdx.x & 63;
   for (int r0 = 0; r0 < requests; r0 += 64) {
@@ -30,7 +31,7 @@ __device__ __forceinline__ bool find_tile(const int32_t* starts, int requests, i
       begin = min(max(starts[r], 0), tokens);
       end = max(min(starts[r + 1], tokens), begin);
     }
-    const int tiles = ((end - begin) * group + kTileRows - 1) / kTileRows;
+    const int tiles = ((end - begin) * group + ROWS - 1) / ROWS;
     int sum = tiles;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
@@ -51,8 +52,21 @@ __device__ __forceinline__ bool find_tile(const int32_t* starts, int requests, i
   return false;
 }
 
+// Workgroups past the last tile clear the padding, the tokens behind the last sequence.
+template <typename T, int D, int ROWS>
+__device__ __forceinline__ void clear_padding(const Prompt<T>& a, int group, int head, int rank) {
+  constexpr int kChunks = Shape<T, D>::kChunks;
+  const int last = a.requests > 0 ? min(max(a.starts[a.requests], 0), (int)a.tokens) : 0;
+  const int rows = (int)(a.tokens - last) * group;
+  for (int i = threadIdx.x; i < ROWS * kChunks; i += kThreads) {
+    const int row = rank * ROWS + i / kChunks;
+    if (row < rows)
+      *reinterpret_cast<u32x4*>(a.out.p + (last + row / group) * a.out.stride + (head * group + row % group) * D + i % kChunks * (16 / (int)sizeof(T))) = u32x4{0u, 0u, 0u, 0u};
+  }
+}
+
 template <typename T, int D>
-__global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void prompt_kernel(const Prompt<T> a, int group) {
+__global__ __launch_bounds__(kThreads, 2) void prompt_kernel(const Prompt<T> a, int group) {
   using S = Shape<T, D>;
   constexpr int kTile = kTileKeys * S::kRow;
   __shared__ __align__(1024) uint8_t lds[4 * kTile];
@@ -61,17 +75,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void prompt_kerne
   const int head = (int)blockIdx.x % a.kv_heads;
   int rank = (int)blockIdx.x / a.kv_heads;
   Place at;
-  if (!find_tile(a.starts, (int)a.requests, (int)a.tokens, group, &rank, &at)) {
-    // workgroups past the last tile clear the padding, tokens behind the last sequence
-    const int last = a.requests > 0 ? min(max(a.starts[a.requests], 0), (int)a.tokens) : 0;
-    const int rows = (int)(a.tokens - last) * group;
-    for (int i = threadIdx.x; i < kTileRows * S::kChunks; i += kThreads) {
-      const int row = rank * kTileRows + i / S::kChunks;
-      if (row < rows)
-        *reinterpret_cast<u32x4*>(a.out.p + (last + row / group) * a.out.stride + (head * group + row % group) * D + i % S::kChunks * (16 / (int)sizeof(T))) = u32x4{0u, 0u, 0u, 0u};
-    }
-    return;
-  }
+  if (!find_tile<kTileRows>(a.starts, (int)a.requests, (int)a.tokens, group, &rank, &at)) return clear_padding<T, D, kTileRows>(a, group, head, rank);
   // longest rows first: what is left at the end of the grid is short
   const int row0 = (at.tiles - 1 - at.tile) * kTileRows, rows = (at.end - at.begin) * group;
   const int row = row0 + 32 * wave + (lane & 31);
@@ -120,13 +124,63 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void prompt_kerne
   r.store(a.out.p + line * a.out.stride + column, present, l != 0.0f ? 1.0f / l : 0.0f, lane);
 }
 
+// 32 rows a workgroup, whose wavefronts share out the keys.
+template <typename T, int D>
+__global__ __launch_bounds__(kThreads, 1) void prompt_small_kernel(const Prompt<T> a, int group) {
+  using S = Shape<T, D>;
+  __shared__ __align__(1024) uint8_t lds[kWaves * 64 * S::kRow];
+  __shared__ float2 ml[kWaves * 32];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int head = (int)blockIdx.x % a.kv_heads;
+  int rank = (int)blockIdx.x / a.kv_heads;
+  Place at;
+  if (!find_tile<32>(a.starts, (int)a.requests, (int)a.tokens, group, &rank, &at)) return clear_padding<T, D, 32>(a, group, head, rank);
+  const int row0 = (at.tiles - 1 - at.tile) * 32, rows = (at.end - at.begin) * group;
+  const int row = row0 + (lane & 31), token = row / group;
+  const bool present = row < rows;
+  const int last = present ? token : -1;
+  const int first = __builtin_amdgcn_readfirstlane(row0 / group);                           // seen by every row
+  const int keys = __builtin_amdgcn_readfirstlane((min(row0 + 32, rows) - 1) / group + 1);  // that some row sees
+  Rows32<T, D> r;
+  r.load_query(a.q.p + (at.begin + token) * a.q.stride + (head * group + row - token * group) * D, present, lane);
+  const Loader<T, D> load_k(lane, (uint32_t)(sizeof(T) * a.k.stride)), load_v(lane, (uint32_t)(sizeof(T) * a.v.stride));
+  auto walk = [&](auto careful) {
+    r.start(lane);
+    walk_private<decltype(careful)::value>(r, lds, load_k, load_v, wave, kWaves, 0, keys, first, last, a.scale * kLog2e, lane, [&](int j) {
+      const int count = min(keys - j, 16);
+      auto bytes = [&](int64_t stride) { return count > 0 ? (uint32_t)(sizeof(T) * ((count - 1) * (uint32_t)stride + D)) : 0u; };
+      return Group<T>{a.k.p + (at.begin + j) * a.k.stride + head * D, a.v.p + (at.begin + j) * a.v.stride + head * D, bytes(a.k.stride), bytes(a.v.stride), false};
+    });
+  };
+  walk(std::false_type{});
+  if (__builtin_amdgcn_ballot_w64(present && r.spoiled()) != 0) walk(std::true_type{});
+  join_waves<kWaves>(r, lds, ml, min(rows - row0, 32), wave, lane, [&](int of, int d, f32x4 o, float, float l) {
+    const float by = l != 0.0f ? 1.0f / l : 0.0f;
+    const int index = row0 + of, t = index / group;
+    T* to = a.out.p + (at.begin + t) * a.out.stride + (head * group + index - t * group) * D + d;
+    if constexpr (sizeof(T) == 2) *reinterpret_cast<u32x2*>(to) = u32x2{pack_bf16x2(o[0] * by, o[1] * by), pack_bf16x2(o[2] * by, o[3] * by)};
+    else *reinterpret_cast<f32x4*>(to) = f32x4{o[0] * by, o[1] * by, o[2] * by, o[3] * by};
+  });
+}
+
+// Binary32 products take 16 times as long as bf16's, so that a workgroup of 128 rows is long and
+// there are few: 32 rows a workgroup, its wavefronts sharing out the keys.
+template <int D>
+void launch_kernel(const Prompt<float>& a, int group, hipStream_t stream) {
+  const int64_t tiles = (a.tokens * group + 31) / 32 + a.requests;
+  prompt_small_kernel<float, D><<<dim3((unsigned)(tiles * a.kv_heads)), kThreads, 0, stream>>>(a, group);
+}
+template <int D>
+void launch_kernel(const Prompt<uint16_t>& a, int group, hipStream_t stream) {
+  const int64_t tiles = (a.tokens * group + kTileRows - 1) / kTileRows + a.requests;
+  prompt_kernel<uint16_t, D><<<dim3((unsigned)(tiles * a.kv_heads)), kThreads, 0, stream>>>(a, group);
+}
+
 template <typename T>
 hipError_t launch(const Prompt<T>& a, int head_dim, hipStream_t stream) {
   const int group = a.q_heads / a.kv_heads;
-  const int64_t tiles = (a.tokens * group + kTileRows - 1) / kTileRows + a.requests;
-  const dim3 grid((unsigned)(tiles * a.kv_heads));
-  if (head_dim == 64) prompt_kernel<T, 64><<<grid, kThreads, 0, stream>>>(a, group);
-  else prompt_kernel<T, 128><<<grid, kThreads, 0, stream>>>(a, group);
+  if (head_dim == 64) launch_kernel<64>(a, group, stream);
+  else launch_kernel<128>(a, group, stream);
   return hipGetLastError();
 }
 

@@ -461,5 +461,95 @@ __device__ __forceinline__ void walk_shared(Rows32<T, D>& r, uint8_t* lds, int t
   for (int t = mine; t < tiles; ++t) turn(t, t & 1 ? a : b);       // the others' tiles
 }
 
+// Keys and values of up to 16 keys: where they begin and how many bytes are there.
+template <typename T>
+struct Group {
+  const T* k;
+  const T* v;
+  uint32_t k_bytes, v_bytes;
+  bool absent;
+};
+
+// The same 32 rows in each of `waves` wavefronts, which take keys [lo, hi) 32 at a time in turn,
+// each through its own LDS (64 rows at lds + wave * 64 rows) and without barriers: the next keys are
+// loaded as soon as the scores of these are formed, the next values after the product.
+// `find(first)` is the group of 16 keys that begins at `first`, a multiple of 16; every row sees
+// the keys up to `all`, the lane's row those up to `last`.
+template <bool CAREFUL, typename T, int D, typename Find>
+__device__ __forceinline__ void walk_private(Rows32<T, D>& r, uint8_t* lds, const Loader<T, D>& load_k, const Loader<T, D>& load_v, int wave,
+                                             int waves, int lo, int hi, int all, int last, float scale, int lane, Find find) {
+  using S = Shape<T, D>;
+  if (lo >= hi) return;
+  uint8_t *const k = lds + wave * 4 * S::kGroup, *const v = k + 2 * S::kGroup;
+  int j = (lo & ~15) + 32 * wave;
+  Group<T> now[2] = {find(j), find(j + 16)};
+#pragma unroll
+  for (int g = 0; g < 2; ++g) load_k.keys(describe(now[g].k, now[g].k_bytes), k + g * S::kGroup, lo - (j + 16 * g));
+#pragma unroll
+  for (int g = 0; g < 2; ++g) load_v.values(describe(now[g].v, now[g].v_bytes), v + g * S::kGroup, lo - (j + 16 * g));
+  for (; j < hi; j += 32 * waves) {
+    const int next_j = j + 32 * waves;
+    const Group<T> next[2] = {find(next_j), find(next_j + 16)};
+    const uint32_t absent = (now[0].absent ? 1u : 0u) | (now[1].absent ? 2u : 0u);
+    const bool edge = j + 31 > min(all, hi - 1) || j < lo || absent != 0;
+    landed<2 * S::kLoads>();
+    f32x16 s[1];
+    r.scores(k, s);
+    have_read();
+#pragma unroll
+    for (int g = 0; g < 2; ++g) load_k.keys(describe(next[g].k, next[g].k_bytes), k + g * S::kGroup);
+    if (edge) Rows32<T, D>::template mask<1>(s, lo - j, min(last, hi - 1) - j, absent, lane);
+    r.template raise<1>(s, scale);
+    typename Products<T, D>::template Weights<1> p;
+    r.template weights<1>(s, scale, p);
+    landed<2 * S::kLoads>();
+    r.template add<CAREFUL, 1>(v, p, edge, min(last, hi - 1) - j, lane);
+    have_read();
+#pragma unroll
+    for (int g = 0; g < 2; ++g) load_v.values(describe(next[g].v, next[g].v_bytes), v + g * S::kGroup);
+    now[0] = next[0];
+    now[1] = next[1];
+  }
+  landed<0>();
+}
+
+// What the wavefronts of a workgroup gathered for the same `count` rows, joined through LDS (16-byte
+// pieces swizzled by row) and handed on four outputs at a time: put(row, at, o, m, l).
+template <int WAVES, typename T, int D, typename Put>
+__device__ __forceinline__ void join_waves(const Rows32<T, D>& r, uint8_t* lds, float2* ml, int count, int wave, int lane, Put put) {
+  constexpr int kPieces = D / 4;
+  const float l = sum_across(r.l);
+  __syncthreads();
+  f32x4* const o = reinterpret_cast<f32x4*>(lds);
+  const int n = lane & 31;
+  if (n < count) {
+#pragma unroll
+    for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        o[(wave * 32 + n) * kPieces + ((8 * t + 2 * i + lane / 32) ^ (n % kPieces))] = f32x4{r.o[t][4 * i], r.o[t][4 * i + 1], r.o[t][4 * i + 2], r.o[t][4 * i + 3]};
+    if (lane < 32) ml[wave * 32 + n] = float2{r.m, l};
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < count * kPieces; i += 64 * WAVES) {
+    const int at = i % kPieces, of = i / kPieces;
+    float m = ml[of].x, sum = 0.0f;
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) m = fmaxf(m, ml[w * 32 + of].x);
+    f32x4 all = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+      const float2 x = ml[w * 32 + of];
+      if (x.y == 0.0f) continue;
+      const float by = __builtin_amdgcn_exp2f(x.x - m);
+      const f32x4 y = o[(w * 32 + of) * kPieces + (at ^ (of % kPieces))];
+      sum = __builtin_fmaf(by, x.y, sum);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) all[e] = __builtin_fmaf(by, y[e], all[e]);
+    }
+    put(of, 4 * at, all, m, sum);
+  }
+}
+
 }  // namespace attention
 }  // namespace ssq

@@ -101,7 +101,13 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
     return t.data_ptr()
 
 
+# the current stream's handle without a Stream object around it (2 us less a call)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream(device: torch.device) -> int:
+    if _raw_stream is not None and device.index is not None:
+        return _raw_stream(device.index)
     return torch.cuda.current_stream(device).cuda_stream
 
 
@@ -361,12 +367,18 @@ for _name in ("ssq_qk_norm_rope", "ssq_attention_prompt", "ssq_attention_decode"
 _EXPORTS["ssq_attention_decode_workspace_size"] = (ctypes.c_size_t, [_L, _I, _I, _I, _I, _L, _L])
 
 
-def _entry(name: str, dtype: torch.dtype) -> str:
-    if dtype == torch.bfloat16:
-        return name
-    if dtype == torch.float32:
-        return name + "_f32"
-    raise TypeError("tensors must be bfloat16 or float32")
+_entries: dict = {}
+
+
+def _entry(name: str, dtype: torch.dtype):
+    """The C function for tensors of dtype, and its name."""
+    found = _entries.get((name, dtype))
+    if found is None:
+        if dtype not in (torch.bfloat16, torch.float32):
+            raise TypeError("tensors must be bfloat16 or float32")
+        full = name if dtype == torch.bfloat16 else name + "_f32"
+        found = _entries[name, dtype] = (getattr(lib(), full), full)
+    return found
 
 
 def _heads(t: torch.Tensor, what: str, dtype: torch.dtype, tokens: Optional[int] = None) -> int:
@@ -376,16 +388,18 @@ def _heads(t: torch.Tensor, what: str, dtype: torch.dtype, tokens: Optional[int]
     n, heads, dim = t.shape
     if tokens is not None and n != tokens:
         raise ValueError(f"{what} has {n} tokens, not {tokens}")
-    stride = t.stride()
-    if stride[2] != 1 or stride[1] != dim:
+    rows, between, one = t.stride()
+    if one != 1 or between != dim:
         raise ValueError(f"the heads of a token of {what} must be contiguous")
-    return stride[0] if n > 1 else heads * dim
+    return rows if n > 1 else heads * dim
 
 
 def _flat(t: torch.Tensor, what: str, dtype: torch.dtype, shape: Tuple[int, ...]) -> int:
-    if t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous():
-        raise ValueError(f"{what} must be a contiguous {dtype} tensor of shape {shape}")
-    return _ptr(t)
+    if t.dtype != dtype or t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous {dtype} tensor of shape {tuple(shape)}")
+    if not t.is_cuda:
+        raise ValueError("ssq kernels take GPU tensors only (got a tensor on %s)" % t.device)
+    return t.data_ptr()
 
 
 def ssq_page_tables(held: torch.Tensor, added: torch.Tensor, free_pages: torch.Tensor, table: torch.Tensor,
@@ -398,26 +412,29 @@ def ssq_page_tables(held: torch.Tensor, added: torch.Tensor, free_pages: torch.T
     lens [requests], positions [tokens], slots [tokens], taken after [1], table), all int32;
     ``tokens`` may exceed the sum of ``added`` (padding: position 0, slot -1).  ``out`` = the
     first five reuses buffers."""
-    n, i32, dev = held.shape[0] if held.dim() == 1 else -1, torch.int32, held.device
-    if table.dim() != 2 or table.shape[0] != n or table.dtype != i32 or not table.is_contiguous():
-        raise ValueError("table must be a contiguous int32 [requests, pages] tensor")
+    if held.dim() != 1 or table.dim() != 2:
+        raise ValueError("held must be [requests] and table [requests, pages]")
+    n, width = table.shape
+    i32, dev, one = torch.int32, held.device, (n,)
     if out is None:
         if tokens < 0:
             raise ValueError("tokens must not be negative")
-        starts = torch.empty(n + 1, dtype=i32, device=dev)
-        lens = torch.empty(n, dtype=i32, device=dev)
-        positions = torch.empty(tokens, dtype=i32, device=dev)
-        slots = torch.empty(tokens, dtype=i32, device=dev)
-        after = torch.empty(1, dtype=i32, device=dev)
+        # one allocation, cut up
+        buf = torch.empty(2 * n + 2 * tokens + 2, dtype=i32, device=dev)
+        starts, lens, positions, slots, after = torch.split_with_sizes(buf, (n + 1, n, tokens, tokens, 1))
+        at = _ptr(buf)
+        to = at, at + 4 * (n + 1), at + 4 * (2 * n + 1), at + 4 * (2 * n + 1 + tokens), at + 4 * (2 * n + 1 + 2 * tokens)
     else:
         starts, lens, positions, slots, after = out
-    st = lib().ssq_page_tables(_flat(held, "held", i32, (n,)), _flat(added, "added", i32, (n,)), n,
-                               _flat(free_pages, "free_pages", i32, (free_pages.numel(),)), free_pages.numel(),
-                               None if taken is None else _flat(taken, "taken", i32, (1,)), page_size,
-                               _ptr(table), table.shape[1], tokens, _flat(starts, "starts", i32, (n + 1,)),
-                               _flat(lens, "lens", i32, (n,)), _flat(positions, "positions", i32, (tokens,)),
-                               _flat(slots, "slots", i32, (tokens,)), _flat(after, "taken after", i32, (1,)), _stream(dev))
-    _check("ssq_page_tables", st)
+        to = (_flat(starts, "starts", i32, (n + 1,)), _flat(lens, "lens", i32, one), _flat(positions, "positions", i32, (tokens,)),
+              _flat(slots, "slots", i32, (tokens,)), _flat(after, "taken after", i32, (1,)))
+    fn, name = _entry("ssq_page_tables", torch.bfloat16)
+    st = fn(_flat(held, "held", i32, one), _flat(added, "added", i32, one), n,
+            _flat(free_pages, "free_pages", i32, free_pages.shape[:1]), free_pages.numel(),
+            None if taken is None else _flat(taken, "taken", i32, (1,)), page_size, _flat(table, "table", i32, (n, width)),
+            width, tokens, *to, _stream(dev))
+    if st:
+        _check(name, st)
     return starts, lens, positions, slots, after, table
 
 
@@ -434,7 +451,7 @@ def ssq_qk_norm_rope(q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor, 
     the caches k_pages, v_pages [pages, kv_heads, page_size, head_dim].  ``out`` = (q, k) reuses
     buffers (k may be None with a cache; they may be q and k themselves)."""
     dtype = q.dtype
-    fn = _entry("ssq_qk_norm_rope", dtype)
+    fn, name = _entry("ssq_qk_norm_rope", dtype)
     qs, ks = _heads(q, "q", dtype), _heads(k, "k", dtype, q.shape[0])
     tokens, hq, dim = q.shape
     hk = k.shape[1]
@@ -444,29 +461,33 @@ def ssq_qk_norm_rope(q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor, 
     if cache != (k_pages is not None) or cache != (v_pages is not None) or (cache and v is None):
         raise ValueError("slots, k_pages and v_pages go together, with v")
     vs = pages = page_size = 0
+    vp = sp = kp = pp = None
     if cache:
-        vs = _heads(v, "v", dtype, tokens)
-        if v.shape[1:] != k.shape[1:] or k_pages.dim() != 4 or k_pages.shape[1] != hk or k_pages.shape[3] != dim:
+        vs, vp = _heads(v, "v", dtype, tokens), _ptr(v)
+        if v.shape != k.shape or k_pages.dim() != 4:
             raise ValueError("v must be like k, and the caches [pages, kv_heads, page_size, head_dim]")
-        pages, page_size = k_pages.shape[0], k_pages.shape[2]
-        _flat(k_pages, "k_pages", dtype, (pages, hk, page_size, dim))
-        _flat(v_pages, "v_pages", dtype, (pages, hk, page_size, dim))
-        _flat(slots, "slots", torch.int32, (tokens,))
+        pages, _, page_size, _ = shape = k_pages.shape
+        if shape[1] != hk or shape[3] != dim:
+            raise ValueError("the caches must be [pages, kv_heads, page_size, head_dim] of k's heads")
+        kp, pp = _flat(k_pages, "k_pages", dtype, shape), _flat(v_pages, "v_pages", dtype, shape)
+        sp = _flat(slots, "slots", torch.int32, (tokens,))
     if out is None:
-        q_out = torch.empty((tokens, hq, dim), dtype=dtype, device=q.device)
-        k_out = torch.empty((tokens, hk, dim), dtype=dtype, device=q.device)
+        dev, qos, kos = q.device, hq * dim, hk * dim
+        q_out = torch.empty((tokens, hq, dim), dtype=dtype, device=dev)
+        k_out = torch.empty((tokens, hk, dim), dtype=dtype, device=dev)
     else:
         q_out, k_out = out
         if q_out.shape != q.shape or (k_out is not None and k_out.shape != k.shape):
             raise ValueError("out must be tensors like q and k")
-    qos = _heads(q_out, "q_out", dtype)
-    kos = 0 if k_out is None else _heads(k_out, "k_out", dtype)
-    gains = [None if g is None else _flat(g, "a gain", dtype, (dim,)) for g in (q_gain, k_gain)]
-    st = getattr(lib(), fn)(_ptr(q), qs, _ptr(k), ks, _ptr(v) if cache else None, vs, tokens, hq, hk, dim, *gains, eps,
-                            _flat(positions, "positions", torch.int32, (tokens,)),
-                            _flat(rope, "rope", torch.float32, tuple(rope.shape)), rope.shape[0], _ptr(q_out), qos,
-                            _ptr(k_out), kos, _ptr(slots), _ptr(k_pages), _ptr(v_pages), pages, page_size, _stream(q.device))
-    _check(fn, st)
+        qos = _heads(q_out, "q_out", dtype)
+        kos = 0 if k_out is None else _heads(k_out, "k_out", dtype)
+    st = fn(_ptr(q), qs, _ptr(k), ks, vp, vs, tokens, hq, hk, dim,
+            None if q_gain is None else _flat(q_gain, "q_gain", dtype, (dim,)),
+            None if k_gain is None else _flat(k_gain, "k_gain", dtype, (dim,)), eps,
+            _flat(positions, "positions", torch.int32, (tokens,)), _flat(rope, "rope", torch.float32, (rope.shape[0], dim)),
+            rope.shape[0], _ptr(q_out), qos, _ptr(k_out), kos, sp, kp, pp, pages, page_size, _stream(q.device))
+    if st:
+        _check(name, st)
     return q_out, k_out
 
 
@@ -477,7 +498,7 @@ def ssq_attention_prompt(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, star
     [requests + 1]) holds the first token of each sequence and the end of the last; tokens behind
     it give zeros.  ``scale`` defaults to 1 / sqrt(head_dim)."""
     dtype = q.dtype
-    fn = _entry("ssq_attention_prompt", dtype)
+    fn, name = _entry("ssq_attention_prompt", dtype)
     qs, ks = _heads(q, "q", dtype), _heads(k, "k", dtype, q.shape[0])
     vs = _heads(v, "v", dtype, q.shape[0])
     tokens, hq, dim = q.shape
@@ -487,13 +508,15 @@ def ssq_attention_prompt(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, star
     if starts.dim() != 1 or starts.shape[0] < 1:
         raise ValueError("starts must hold requests + 1 values")
     if out is None:
-        out = torch.empty((tokens, hq, dim), dtype=dtype, device=q.device)
+        out, os_ = torch.empty((tokens, hq, dim), dtype=dtype, device=q.device), hq * dim
     elif out.shape != q.shape:
         raise ValueError("out must be a tensor like q")
-    st = getattr(lib(), fn)(_ptr(q), qs, _ptr(k), ks, _ptr(v), vs,
-                            _flat(starts, "starts", torch.int32, tuple(starts.shape)), starts.shape[0] - 1, tokens, hq, hk,
-                            dim, dim ** -0.5 if scale is None else scale, _ptr(out), _heads(out, "out", dtype), _stream(q.device))
-    _check(fn, st)
+    else:
+        os_ = _heads(out, "out", dtype)
+    st = fn(_ptr(q), qs, _ptr(k), ks, _ptr(v), vs, _flat(starts, "starts", torch.int32, starts.shape), starts.shape[0] - 1,
+            tokens, hq, hk, dim, dim ** -0.5 if scale is None else scale, _ptr(out), os_, _stream(q.device))
+    if st:
+        _check(name, st)
     return out
 
 
@@ -515,7 +538,7 @@ def ssq_attention_decode(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.
     ``workspace`` (uint8, any contents, ``ssq_attention_decode_workspace_size`` bytes) is allocated
     where it is not given; ``scale`` defaults to 1 / sqrt(head_dim)."""
     dtype = q.dtype
-    fn = _entry("ssq_attention_decode", dtype)
+    fn, name = _entry("ssq_attention_decode", dtype)
     if q.dim() != 4 or q.stride(3) != 1 or q.stride(2) != q.shape[3] or (
             q.shape[0] > 1 and q.shape[1] > 1 and q.stride(0) != q.shape[1] * q.stride(1)):
         raise ValueError("q must be [requests, fresh, q_heads, head_dim], its tokens equally far apart and each contiguous")
@@ -535,11 +558,11 @@ def ssq_attention_decode(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.
         if size:
             workspace = torch.empty(size, dtype=torch.uint8, device=q.device)
     stride = q.stride(1) if fresh > 1 else q.stride(0) if n > 1 else hq * dim
-    st = getattr(lib(), fn)(_ptr(q), stride, n, fresh, hq, hk, dim, dim ** -0.5 if scale is None else scale,
-                            _flat(k_pages, "k_pages", dtype, (pages, hk, page_size, dim)),
-                            _flat(v_pages, "v_pages", dtype, (pages, hk, page_size, dim)), pages, page_size,
-                            _flat(table, "table", torch.int32, (n, width)), width, _flat(lens, "lens", torch.int32, (n,)), max_len,
-                            prefix, _ptr(out), hq * dim, _ptr(workspace),
-                            0 if workspace is None else workspace.numel() * workspace.element_size(), _stream(q.device))
-    _check(fn, st)
+    shape = k_pages.shape
+    st = fn(_ptr(q), stride, n, fresh, hq, hk, dim, dim ** -0.5 if scale is None else scale, _flat(k_pages, "k_pages", dtype, shape),
+            _flat(v_pages, "v_pages", dtype, shape), pages, page_size, _flat(table, "table", torch.int32, (n, width)), width,
+            _flat(lens, "lens", torch.int32, (n,)), max_len, prefix, _ptr(out), hq * dim, _ptr(workspace),
+            0 if workspace is None else workspace.numel() * workspace.element_size(), _stream(q.device))
+    if st:
+        _check(name, st)
     return out

@@ -7,8 +7,8 @@
 // * wide: 128 query rows (all requests' new tokens and the group's heads) against a stretch
 //   of the shared prefix, 64 keys at a time through two stages of LDS that the four
 //   wavefronts share.
-// * narrow: up to 32 query rows (one request's; or all, against the prefix, where they are so
-//   few) against a stretch of keys that the four wavefronts take 32 at a time, each through
+// * narrow: up to 32 query rows (one request's; or all requests', against the prefix, where they
+//   are no more than 32 in all, and in binary32) against a stretch of keys that the four wavefronts take 32 at a time, each through
 //   LDS of its own and without barriers: the next keys are loaded as soon as the scores of
 //   these are formed, the next values after the product.  Rows beside the used ones
 //   cost nothing that is scarce here.
@@ -48,7 +48,7 @@ struct Parts {           // of every row: [part][row] and [part][row][D]
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-Plan make_plan(int64_t requests, int fresh, int q_heads, int kv_heads, int64_t max_len, int64_t prefix, bool split) {
+Plan make_plan(int64_t requests, int fresh, int q_heads, int kv_heads, int64_t max_len, int64_t prefix, bool split, bool wide) {
   Plan p = {};
   p.group = q_heads / kv_heads;
   p.rows = (int)(requests * fresh * p.group);
@@ -60,9 +60,9 @@ Plan make_plan(int64_t requests, int fresh, int q_heads, int kv_heads, int64_t m
   constexpr int64_t kGroups = 512;       // two workgroups for each of 256 CUs
   prefix = std::min(prefix, max_len);
   if (requests > 1 && prefix > 0) {
-    p.share = p.rows > kNarrowRows ? kShareWide : kShareNarrow;
-    p.prefix_tiles = p.share == kShareWide ? (int)ceil_div(p.rows, kWideRows) : 1;
-    p.prefix_parts = (int)std::clamp(ceil_div(kGroups / 2, (int64_t)p.prefix_tiles * kv_heads), (int64_t)1,
+    p.share = p.rows > kNarrowRows && wide ? kShareWide : kShareNarrow;
+    p.prefix_tiles = (int)ceil_div(p.rows, p.share == kShareWide ? kWideRows : kNarrowRows);
+    p.prefix_parts = (int)std::clamp(ceil_div(kGroups / 2, ceil_div(p.rows, kWideRows) * kv_heads), (int64_t)1,
                                      std::min<int64_t>(kMaxParts / 2, ceil_div(prefix, 256)));
   } else {
     prefix = 0;
@@ -266,7 +266,10 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void decode_kerne
   if (on_prefix) {
     const int tile = i0 % p.prefix_tiles;
     part = i0 / p.prefix_tiles;
-    if (p.share == kShareWide) return wide<T, D>(a, p, parts, head, tile, part, lds, &spoiled);
+    if constexpr (sizeof(T) == 2) {
+      if (p.share == kShareWide) return wide<T, D>(a, p, parts, head, tile, part, lds, &spoiled);
+    }
+    index0 = tile * kNarrowRows;
     const int per = ((prefix + p.prefix_parts - 1) / p.prefix_parts + kNarrowKeys - 1) / kNarrowKeys * kNarrowKeys;
     range[0].begin = min(part * per, prefix);
     range[0].end = min(range[0].begin + per, prefix);
@@ -340,10 +343,10 @@ size_t part_bytes(const Plan& p, int head_dim) {
 
 template <typename T, int D>
 hipError_t launch(const Decode<T>& a, void* workspace, size_t workspace_bytes, hipStream_t stream) {
-  Plan p = make_plan(a.requests, a.fresh, a.q_heads, a.kv_heads, a.max_len, a.prefix, true);
+  Plan p = make_plan(a.requests, a.fresh, a.q_heads, a.kv_heads, a.max_len, a.prefix, true, sizeof(T) == 2);
   size_t need = part_bytes(p, D);
   if (need > 0 && (workspace == nullptr || workspace_bytes < need)) {
-    p = make_plan(a.requests, a.fresh, a.q_heads, a.kv_heads, a.max_len, a.prefix, false);
+    p = make_plan(a.requests, a.fresh, a.q_heads, a.kv_heads, a.max_len, a.prefix, false, false);
     need = 0;
   }
   Parts parts = {nullptr, nullptr};
@@ -362,7 +365,7 @@ hipError_t launch(const Decode<T>& a, void* workspace, size_t workspace_bytes, h
 
 size_t attention_decode_workspace_bytes(int64_t requests, int fresh, int q_heads, int kv_heads, int head_dim,
                                         int64_t max_len, int64_t prefix) {
-  return attention::part_bytes(attention::make_plan(requests, fresh, q_heads, kv_heads, max_len, prefix, true), head_dim);
+  return attention::part_bytes(attention::make_plan(requests, fresh, q_heads, kv_heads, max_len, prefix, true, true), head_dim);
 }
 
 template <typename T>

@@ -27,6 +27,7 @@ namespace {
 constexpr int kWaves = 4, kThreads = 64 * kWaves, kWideRows = 32 * kWaves, kWideKeys = 64, kNarrowRows = 32;
 constexpr int kNarrowKeys = 32 * kWaves;              // keys that a narrow workgroup takes at a time
 constexpr int kMaxParts = 64;
+constexpr int64_t kWaveJoinRows = 1536;               // rows of out from which a wavefront joins a row
 
 enum Share : int { kShareNone = 0, kShareWide, kShareNarrow };
 
@@ -290,16 +291,17 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void decode_kerne
   narrow<T, D>(a, p, parts, head, request, index0, range, part, lds, ml);
 }
 
-// One row of out from its parts, by a workgroup: D / 4 lanes hold the row, and the groups of so
-// many lanes take the parts in turn, so that all their loads are under way at once.
-template <typename T, int D>
+// One row of out from its parts, by R lanes, a wavefront or a workgroup of them: D / 4 lanes hold the
+// row, and the groups of so many lanes take the parts in turn, so that their loads are under way
+// together.
+template <typename T, int D, int R>
 __global__ __launch_bounds__(kThreads) void join_kernel(const Decode<T> a, int64_t line_rows, int count, const Parts parts) {
-  constexpr int kLanes = D / 4, kGroups = kThreads / kLanes;
-  __shared__ f32x4 sums[kGroups][kLanes];
-  const int lane = threadIdx.x & 63, at = (int)threadIdx.x % kLanes, group = (int)threadIdx.x / kLanes;
-  const int64_t row = blockIdx.x;
+  constexpr int kLanes = D / 4, kGroups = R / kLanes;
+  const int lane = threadIdx.x & 63, at = (int)threadIdx.x % kLanes, group = (int)threadIdx.x % R / kLanes;
+  const int64_t row = blockIdx.x * (int64_t)(kThreads / R) + threadIdx.x / R;
+  if (row >= line_rows) return;               // whole wavefronts; none where a workgroup holds a row
   const float* from = parts.o + row * D + 4 * at;
-  constexpr int kAhead = 4;
+  constexpr int kAhead = R == 64 ? 8 : 4;
   f32x4 o[kAhead];
 #pragma unroll
   for (int i = 0; i < kAhead; ++i) {
@@ -325,13 +327,22 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const Decode<T> a, int64
 #pragma unroll
     for (int e = 0; e < 4; ++e) sum[e] = __builtin_fmaf(w, y[e], sum[e]);
   }
-  sums[group][at] = sum;
-  __syncthreads();
+  if constexpr (R == 64) {
+#pragma unroll
+    for (int d = kLanes; d < 64; d <<= 1)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum[e] += __shfl_xor(sum[e], d, 64);
+  } else {
+    __shared__ f32x4 sums[kGroups][kLanes];
+    sums[group][at] = sum;
+    __syncthreads();
+    if (group != 0) return;
+#pragma unroll
+    for (int g = 1; g < kGroups; ++g)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum[e] += sums[g][at][e];
+  }
   if (group != 0) return;
-#pragma unroll
-  for (int g = 1; g < kGroups; ++g)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) sum[e] += sums[g][at][e];
   const int64_t line = row / a.q_heads;
   const Row to = {true, line, (int)(row - line * a.q_heads), 0};
   put<T, D>(a, Plan{}, Parts{nullptr, nullptr}, 0, to, 4 * at, sum, 0.0f, l);
@@ -356,7 +367,14 @@ hipError_t launch(const Decode<T>& a, void* workspace, size_t workspace_bytes, h
   }
   const int64_t prefix_groups = p.prefix_groups(), own_groups = a.requests * p.own_tiles * p.own_parts;
   decode_kernel<T, D><<<dim3((unsigned)((prefix_groups + own_groups) * a.kv_heads)), kThreads, 0, stream>>>(a, p, parts, (int)prefix_groups, (int)own_groups);
-  if (need > 0) join_kernel<T, D><<<dim3((unsigned)p.line_rows), kThreads, 0, stream>>>(a, p.line_rows, p.parts(), parts);
+  if (need > 0) {
+    // A wavefront a row where the rows fill the chip (2560 rows of 7 parts: a step of 20.3 us against
+    // 21.2 with a workgroup a row), a workgroup a row where they do not (32 rows of 32 parts: 18.9
+    // against 21.9; equal at about 1000 rows).
+    constexpr int kPerGroup = kThreads / 64;
+    if (p.line_rows >= kWaveJoinRows) join_kernel<T, D, 64><<<dim3((unsigned)((p.line_rows + kPerGroup - 1) / kPerGroup)), kThreads, 0, stream>>>(a, p.line_rows, p.parts(), parts);
+    else join_kernel<T, D, kThreads><<<dim3((unsigned)p.line_rows), kThreads, 0, stream>>>(a, p.line_rows, p.parts(), parts);
+  }
   return hipGetLastError();
 }
 

@@ -368,6 +368,7 @@ _EXPORTS["ssq_attention_decode_workspace_size"] = (ctypes.c_size_t, [_L, _I, _I,
 
 
 _entries: dict = {}
+_PACKED = torch.contiguous_format       # of outputs, whatever their inputs' strides (empty_like takes half of empty's time)
 
 
 def _entry(name: str, dtype: torch.dtype):
@@ -472,9 +473,8 @@ def ssq_qk_norm_rope(q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor, 
         kp, pp = _flat(k_pages, "k_pages", dtype, shape), _flat(v_pages, "v_pages", dtype, shape)
         sp = _flat(slots, "slots", torch.int32, (tokens,))
     if out is None:
-        dev, qos, kos = q.device, hq * dim, hk * dim
-        q_out = torch.empty((tokens, hq, dim), dtype=dtype, device=dev)
-        k_out = torch.empty((tokens, hk, dim), dtype=dtype, device=dev)
+        qos, kos = hq * dim, hk * dim
+        q_out, k_out = torch.empty_like(q, memory_format=_PACKED), torch.empty_like(k, memory_format=_PACKED)
     else:
         q_out, k_out = out
         if q_out.shape != q.shape or (k_out is not None and k_out.shape != k.shape):
@@ -508,7 +508,7 @@ def ssq_attention_prompt(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, star
     if starts.dim() != 1 or starts.shape[0] < 1:
         raise ValueError("starts must hold requests + 1 values")
     if out is None:
-        out, os_ = torch.empty((tokens, hq, dim), dtype=dtype, device=q.device), hq * dim
+        out, os_ = torch.empty_like(q, memory_format=_PACKED), hq * dim
     elif out.shape != q.shape:
         raise ValueError("out must be a tensor like q")
     else:
@@ -550,7 +550,7 @@ def ssq_attention_decode(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.
         raise ValueError("table must be a contiguous int32 [requests, pages] tensor")
     width = table.shape[1]
     if out is None:
-        out = torch.empty((n, fresh, hq, dim), dtype=dtype, device=q.device)
+        out = torch.empty_like(q, memory_format=_PACKED)
     elif out.shape != q.shape or out.dtype != dtype or not out.is_contiguous():
         raise ValueError("out must be a contiguous tensor like q")
     if workspace is None:

@@ -6,6 +6,7 @@
 // heads share every key and value that is loaded and the causal edge is one tile wide.  It
 // walks the stretch's keys 64 at a time through two stages of LDS, the next tile on its way
 // while this one is used.
+#include <algorithm>
 #include <type_traits>
 
 #include "attention_tiles.h"
@@ -32,12 +33,13 @@ __device__ __forceinline__ bool find_tile(const int32_t* starts, int requests, i
       end = max(min(starts[r + 1], tokens), begin);
     }
     const int tiles = ((end - begin) * group + ROWS - 1) / ROWS;
-    int sum = tiles;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int x = __shfl_up(sum, o, 64);
-      if (lane >= o) sum += x;
-    }
+    int sum = tiles;                                   // with those of the lanes before it: DPP row shifts and broadcasts
+    sum += __builtin_amdgcn_update_dpp(0, sum, 0x111, 0xF, 0xF, true);
+    sum += __builtin_amdgcn_update_dpp(0, sum, 0x112, 0xF, 0xF, true);
+    sum += __builtin_amdgcn_update_dpp(0, sum, 0x114, 0xF, 0xF, true);
+    sum += __builtin_amdgcn_update_dpp(0, sum, 0x118, 0xF, 0xF, true);
+    sum += __builtin_amdgcn_update_dpp(0, sum, 0x142, 0xA, 0xF, true);
+    sum += __builtin_amdgcn_update_dpp(0, sum, 0x143, 0xC, 0xF, true);
     const uint64_t past = __builtin_amdgcn_ballot_w64(sum > *rank);
     if (past != 0) {
       const int found = __builtin_ctzll(past);
@@ -126,7 +128,7 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(const Prompt<T> a, 
 
 // 32 rows a workgroup, whose wavefronts share out the keys.
 template <typename T, int D>
-__global__ __launch_bounds__(kThreads, 1) void prompt_small_kernel(const Prompt<T> a, int group) {
+__global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void prompt_small_kernel(const Prompt<T> a, int group) {
   using S = Shape<T, D>;
   __shared__ __align__(1024) uint8_t lds[kWaves * 64 * S::kRow];
   __shared__ float2 ml[kWaves * 32];
@@ -163,15 +165,39 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_small_kernel(const Prompt<
   });
 }
 
+template <typename T>
+int64_t small_groups(const Prompt<T>& a, int group) { return ((a.tokens * group + 31) / 32 + a.requests) * a.kv_heads; }
+template <typename T, int D>
+void launch_small(const Prompt<T>& a, int group, hipStream_t stream) {
+  prompt_small_kernel<T, D><<<dim3((unsigned)small_groups(a, group)), kThreads, 0, stream>>>(a, group);
+}
+
 // Binary32 products take 16 times as long as bf16's, so that a workgroup of 128 rows is long and
 // there are few: 32 rows a workgroup, its wavefronts sharing out the keys.
 template <int D>
 void launch_kernel(const Prompt<float>& a, int group, hipStream_t stream) {
-  const int64_t tiles = (a.tokens * group + 31) / 32 + a.requests;
-  prompt_small_kernel<float, D><<<dim3((unsigned)(tiles * a.kv_heads)), kThreads, 0, stream>>>(a, group);
+  launch_small<float, D>(a, group, stream);
+}
+
+// In bf16 that form loads each key four times as often.  It pays where its workgroups are all
+// resident at once and sequences are long for their number, as with the few key/value heads of
+// a small model or of a shard: there a row tile's time is one walk over its keys, which the
+// wavefronts then share (us, 128 rows -> 32 rows a workgroup, one sequence):
+//   2 kv heads of 128, group 4: 400 tokens 10.7 -> 9.7, 1000 20.1 -> 13.5, 3000 49.8 -> 36.8
+//   8 kv heads of 128, group 4: 400 tokens 11.1 -> 11.5, 1000 21.4 -> 26.5: not taken
+//   8 kv heads of 64, group 1: 100 tokens 5.5 -> 4.9, 1000 14.9 -> 9.6
+//   8 kv heads of 64, group 4: 700 tokens 11.6 -> 10.1, 1000 15.3 -> 17.4: not taken
+// and short sequences (16 of 47 tokens in the mean, 2 kv heads of 128: 6.2 -> 7.2) lose.
+template <int D>
+bool prefers_small(const Prompt<uint16_t>& a, int group) {
+  if (a.requests == 0) return false;
+  const int64_t groups = small_groups(a, group), mean = a.tokens / a.requests;
+  constexpr int64_t kResident = 3 * 256;
+  return D == 64 ? mean >= 96 && groups <= std::min(kResident, mean * 8 / 7) : mean >= 320 && groups <= std::min(kResident, mean);
 }
 template <int D>
 void launch_kernel(const Prompt<uint16_t>& a, int group, hipStream_t stream) {
+  if (prefers_small<D>(a, group)) return launch_small<uint16_t, D>(a, group, stream);
   const int64_t tiles = (a.tokens * group + kTileRows - 1) / kTileRows + a.requests;
   prompt_kernel<uint16_t, D><<<dim3((unsigned)(tiles * a.kv_heads)), kThreads, 0, stream>>>(a, group);
 }

@@ -147,6 +147,40 @@ def test_prompt_writes_only_its_rows():
     assert (wide[:, 0] == 7).all() and (wide[:, hq + 1:] == 7).all()
 
 
+# Few rows and long sequences: in bf16 the kernel of 32 rows a workgroup, its neighbours around the rule
+FEW = [
+    ([97], (4, 4, 64)), ([430], (4, 1, 128)), ([129, 0, 300], (8, 2, 64)), ([321], (8, 2, 128)),
+    ([800], (6, 1, 128)), ([1100, 3], (14, 2, 64)), ([333, 340], (2, 2, 128)), ([95], (4, 4, 64)), ([319], (8, 2, 128)),
+]
+
+
+@pytest.mark.parametrize("i", range(len(FEW)))
+def test_prompt_few_rows(i):
+    lens, heads = FEW[i]
+    q, k, v = prompt_inputs(lens, heads, BF, 80 + i, fused=i % 2 == 0, pad=(0, 35)[i % 2])
+    wide = torch.full((len(q), heads[0] + 2, heads[2]), 7.0, dtype=BF, device="cuda")
+    out = ssq.ssq_attention_prompt(q, k, v, ints(A.starts_of(lens)), out=wide[:, 1:heads[0] + 1])
+    ref, size, eps = A.prompt_reference(q, k, v, lens)
+    A.check(out, ref, size, eps, f"{lens} {heads}")
+    assert not out[sum(lens):].any() and (wide[:, 0] == 7).all() and (wide[:, -1] == 7).all()
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("heads", [(8, 2, 128), (6, 6, 64)])
+def test_prompt_few_rows_hidden_keys_have_no_influence(bad, heads):
+    lens = [400, 350]
+    q, k, v = prompt_inputs(lens, heads, BF, 90, pad=11)
+    ref, size, eps = A.prompt_reference(q, k, v, lens)
+    k, v = k.clone(), v.clone()
+    for t in (37, 161, 400 + 77, 755):
+        k[t, :, ::3] = bad
+        v[t, :, 1::2] = bad
+    out = ssq.ssq_attention_prompt(q, k, v, ints(A.starts_of(lens)))
+    for a, b in ((0, 37), (400, 477)):
+        A.check(out[a:b], ref[a:b], size[a:b], eps[a:b], f"{bad} {a}")
+    assert not out[477:750].isfinite().all() and not out[750:].any()
+
+
 def test_prompt_scale_and_repeat():
     lens = [90, 33]
     q, k, v = prompt_inputs(lens, (8, 2, 64), BF, 9)

@@ -99,12 +99,6 @@ __device__ __forceinline__ int64_t group_offset(const Decode<T>& a, int head, in
   return (((page * a.kv_heads + head) << a.cache.page_shift) + (j & ((1 << a.cache.page_shift) - 1))) * D;
 }
 
-__device__ __forceinline__ int wave_min(int v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v = min(v, __shfl_xor(v, o, 64));
-  return __builtin_amdgcn_readfirstlane(v);
-}
-
 template <typename T>
 __device__ __forceinline__ int request_len(const Decode<T>& a, int request) {
   const int64_t room = min(a.max_len, a.table_stride << a.cache.page_shift);
@@ -310,13 +304,9 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const Decode<T> a, int64
   }
   // every wavefront forms the parts' weights, for itself
   const float2 x = lane < count ? parts.ml[lane * line_rows + row] : float2{-FLT_MAX, 0.0f};
-  float m = x.y != 0.0f ? x.x : -FLT_MAX;
-#pragma unroll
-  for (int d = 32; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor(m, d, 64));
+  const float m = wave_max(x.y != 0.0f ? x.x : -FLT_MAX);
   const float by = x.y != 0.0f ? __builtin_amdgcn_exp2f(x.x - m) : 0.0f;
-  float l = by * x.y;
-#pragma unroll
-  for (int d = 32; d > 0; d >>= 1) l += __shfl_xor(l, d, 64);
+  const float l = wave_sum(by * x.y);
   f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
   for (int i = 0; i < kMaxParts / kGroups; ++i) {

@@ -22,6 +22,8 @@
 
 #include <float.h>
 
+#include <type_traits>
+
 #include "attention_internal.h"
 #include "mfma_dequant.h"
 
@@ -64,6 +66,42 @@ __device__ __forceinline__ float max_across(float v) {       // of lane and lane
 __device__ __forceinline__ float sum_across(float v) {
   const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
   return __uint_as_float(s[0]) + __uint_as_float(s[1]);
+}
+
+// A reduction over the wavefront's 64 lanes in six DPP moves (shifts within rows of 16 lanes, then
+// broadcasts across them), an eighth of the latency of as many exchanges through LDS; lanes that a
+// move gives nothing keep their own value, twice.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t dpp_or_own(uint32_t v) { return __builtin_amdgcn_update_dpp(v, v, CTRL, ROWS, 0xF, false); }
+template <typename Op>
+__device__ __forceinline__ uint32_t wave_reduce(uint32_t v, Op op) {
+  v = op(v, dpp_or_own<0x111, 0xF>(v));
+  v = op(v, dpp_or_own<0x112, 0xF>(v));
+  v = op(v, dpp_or_own<0x114, 0xF>(v));
+  v = op(v, dpp_or_own<0x118, 0xF>(v));
+  v = op(v, dpp_or_own<0x142, 0xA>(v));
+  v = op(v, dpp_or_own<0x143, 0xC>(v));
+  return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
+}
+__device__ __forceinline__ int wave_min(int v) {
+  return (int)wave_reduce((uint32_t)v, [](uint32_t x, uint32_t y) { return (uint32_t)min((int)x, (int)y); });
+}
+__device__ __forceinline__ float wave_max(float v) {
+  return __uint_as_float(wave_reduce(__float_as_uint(v), [](uint32_t x, uint32_t y) { return __float_as_uint(fmaxf(__uint_as_float(x), __uint_as_float(y))); }));
+}
+// Sums need zeros where a move gives nothing.
+__device__ __forceinline__ float wave_sum(float v) {
+  auto step = [&](auto ctrl, auto rows) {
+    v += __uint_as_float(__builtin_amdgcn_update_dpp(0u, __float_as_uint(v), decltype(ctrl)::value, decltype(rows)::value, 0xF, true));
+  };
+  std::integral_constant<int, 0xF> all;
+  step(std::integral_constant<int, 0x111>(), all);
+  step(std::integral_constant<int, 0x112>(), all);
+  step(std::integral_constant<int, 0x114>(), all);
+  step(std::integral_constant<int, 0x118>(), all);
+  step(std::integral_constant<int, 0x142>(), std::integral_constant<int, 0xA>());
+  step(std::integral_constant<int, 0x143>(), std::integral_constant<int, 0xC>());
+  return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(v), 63));
 }
 
 // Every load but the last N has landed, for this wavefront: what it reads from LDS is read after.

@@ -49,6 +49,25 @@ struct Parts {           // of every row: [part][row] and [part][row][D]
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
+// Parts of the prefix, for `tiles` workgroups a part: the quickest by a fit of its time (us).  A
+// tile of 64 keys takes a workgroup 1.1 where it has a CU to itself and 1.57 where it shares one, of
+// 512 places in all; a workgroup's start and end take about 4 tiles' time; and every part of a row
+// is written and read again.  So parts grow until the CUs have a workgroup each; beyond that, only
+// where whole tiles fill them badly (18 x 8 tiles behind 9589 keys, 79 requests of 7 tokens: 3 parts
+// 115 us, 2 parts 147, 4 parts 138; 2 x 8 tiles behind 8192 keys: 16 parts 41.8 us, 24 parts 46.3).
+int choose_prefix_parts(int64_t tiles, int64_t prefix, int64_t line_rows) {
+  const int64_t most = std::min<int64_t>(kMaxParts / 2, ceil_div(prefix, 256));
+  int best = 1;
+  double best_us = 0.0;
+  for (int n = 1; n <= most; ++n) {
+    const int64_t groups = tiles * n;
+    const double tile_us = groups <= 256 ? 1.1 : 1.57 * (double)ceil_div(groups, 512);
+    const double us = tile_us * (double)(ceil_div(ceil_div(prefix, n), kWideKeys) + 4) + 0.25e-3 * (double)(n * line_rows);
+    if (n == 1 || us < best_us) best = n, best_us = us;
+  }
+  return best;
+}
+
 Plan make_plan(int64_t requests, int fresh, int q_heads, int kv_heads, int64_t max_len, int64_t prefix, bool split, bool wide) {
   Plan p = {};
   p.group = q_heads / kv_heads;
@@ -63,8 +82,7 @@ Plan make_plan(int64_t requests, int fresh, int q_heads, int kv_heads, int64_t m
   if (requests > 1 && prefix > 0) {
     p.share = p.rows > kNarrowRows && wide ? kShareWide : kShareNarrow;
     p.prefix_tiles = (int)ceil_div(p.rows, p.share == kShareWide ? kWideRows : kNarrowRows);
-    p.prefix_parts = (int)std::clamp(ceil_div(kGroups / 2, ceil_div(p.rows, kWideRows) * kv_heads), (int64_t)1,
-                                     std::min<int64_t>(kMaxParts / 2, ceil_div(prefix, 256)));
+    p.prefix_parts = choose_prefix_parts(ceil_div(p.rows, kWideRows) * kv_heads, prefix, p.line_rows);
   } else {
     prefix = 0;
   }
@@ -249,12 +267,14 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void decode_kerne
   __shared__ float2 ml[kWaves * 32];
   __shared__ int spoiled;
   const int prefix = (int)min(a.prefix, min(a.max_len, a.table_stride << a.cache.page_shift));
-  // the heads in turn; of the rest, work on the prefix (arithmetic) and on the requests' own keys
-  // (memory) in turn while there are both, so that a CU has some of each
+  // The heads in turn; of the rest, work on the prefix (arithmetic, and long) before the requests' own
+  // keys (memory): workgroups go to the XCDs, their shader engines and CUs in turn, so that each CU
+  // gets some of both.  With the two kinds taken in turn some shader engines got long ones only, and
+  // held up all that came after (79 requests of 7 tokens
+  // behind 9589 keys: 227 us against 147).
   const int head = (int)blockIdx.x % a.kv_heads, turn = (int)blockIdx.x / a.kv_heads;
-  const int both = 2 * min(prefix_groups, own_groups);
-  const bool on_prefix = turn < both ? turn % 2 == 0 : prefix_groups > own_groups;
-  const int i0 = turn < both ? turn / 2 : turn - both / 2;
+  const bool on_prefix = turn < prefix_groups;
+  const int i0 = on_prefix ? turn : turn - prefix_groups;
   // what lies in the prefix comes from the first request's pages, shared or not
   Range range[2] = {{a.table, 0, 0}, {a.table, 0, 0}};
   int request = -1, index0 = 0, part;

@@ -293,6 +293,23 @@ def test_decode_lengths_are_bounded():
     A.check(run_decode(q, k, v, table, lens, 0, max_len=100000), ref, size, eps, "a wide bound")
 
 
+# Many rows behind a longer prefix: several row tiles and parts, their numbers not those of the chip
+MANY = [
+    ([900 + 7 * i for i in range(30)], 3, 890, 32, (9, 3, 128)),
+    ([1300 + i for i in range(45)], 5, 1281, 64, (8, 1, 64)),
+    ([640 + (37 * i) % 300 for i in range(21)], 1, 640, 16, (28, 7, 64)),
+]
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("i", range(len(MANY)))
+def test_decode_many_rows_behind_a_prefix(i, dtype):
+    lens, fresh, prefix, page, heads = MANY[i]
+    q, k, v, table, lens = cache_inputs(lens, fresh, prefix, page, heads, dtype, 100 + i, poison=float("nan"))
+    ref, size, eps = A.decode_reference(q, k, v, table, lens, max(lens), prefix)
+    A.check(run_decode(q, k, v, table, lens, prefix), ref, size, eps, f"{heads} {dtype}")
+
+
 @pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("bad", [float("nan"), float("inf")])
 def test_decode_later_drafts_have_no_influence(dtype, bad):

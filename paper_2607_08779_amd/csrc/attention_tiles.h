@@ -199,6 +199,11 @@ struct Products<uint16_t, D> {
   static __device__ __forceinline__ void set(Weights<KT>& p, int kt, int i, float a, float b) {
     p.w[2 * kt + i / 4][i % 4] = pack_bf16x2(a, b);
   }
+  template <int KT>
+  static __device__ __forceinline__ float add_weights(const Weights<KT>& p, int kt, int i, float sum) {
+    const uint32_t pair = p.w[2 * kt + i / 4][i % 4];      // a value first: a bit cast of a vector's element casts the vector
+    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pair), __builtin_bit_cast(bf16x2, 0x3F803F80u), sum, false);
+  }
   // V^T of 16 keys (chunk c of the tile) and 32 outputs (tile t), as an A operand.
   __device__ __forceinline__ bf16x8 value(const uint8_t* values, int c, int t) const {
     s16x4 d[2];
@@ -272,6 +277,10 @@ struct Products<float, D> {
   static __device__ __forceinline__ void set(Weights<KT>& p, int kt, int i, float a, float b) {
     p.w[kt][2 * i] = a;
     p.w[kt][2 * i + 1] = b;
+  }
+  template <int KT>
+  static __device__ __forceinline__ float add_weights(const Weights<KT>& p, int kt, int i, float sum) {
+    return sum + (p.w[kt][2 * i] + p.w[kt][2 * i + 1]);
   }
   template <int KT>
   __device__ __forceinline__ void accumulate(const uint8_t* values, const Weights<KT>& p, f32x16 (&o)[S::kOut]) const {
@@ -377,20 +386,22 @@ struct Rows32 {
     }
   }
 
-  // Weights of 32 KT keys from their scores, and the running sum.
+  // Weights of 32 KT keys from their scores, and the running sum.  The sum is that of the weights as
+  // the product takes them, so that their rounding is one of weights that still add up to one
+  // (in bf16: a row of one or a few keys comes out as exact as its values are).
   template <int KT>
   __device__ __forceinline__ void weights(const f32x16 (&s)[KT], float scale, typename P::template Weights<KT>& p) {
-    float sum = 0.0f;
+    float sum[2] = {0.0f, 0.0f};
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const float a = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kt][2 * i], scale, -m));
         const float b = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kt][2 * i + 1], scale, -m));
-        sum += a + b;
         P::set(p, kt, i, a, b);
+        sum[i % 2] = P::add_weights(p, kt, i, sum[i % 2]);
       }
-    l += sum;
+    l += sum[0] + sum[1];
   }
 
   // The product with the values key by key, adding only to the rows that see the key: a weight

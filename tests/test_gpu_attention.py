@@ -190,6 +190,17 @@ def test_prompt_scale_and_repeat():
     assert torch.equal(out, again)
 
 
+def test_rows_of_one_key_give_its_value():
+    """The weights' rounding cancels in a row of one key: w v / w, to within binary32, is v in bf16."""
+    q, k, v = prompt_inputs([1] * 200, (8, 2, 128), BF, 95)
+    out = ssq.ssq_attention_prompt(q * 3, k, v, torch.arange(201, device="cuda", dtype=torch.int32))
+    assert torch.equal(out, v.repeat_interleave(4, 1))
+    q, kp, vp, table, lens = cache_inputs([1] * 50, 1, 0, 16, (8, 2, 64), BF, 96)
+    out = run_decode(q * 3, kp, vp, table, lens, 0)
+    want = vp[table[:, 0].long().cuda(), :, 0]
+    assert torch.equal(out[:, 0], want.repeat_interleave(4, 1))
+
+
 # --- decoding -----------------------------------------------------------------------------------
 
 def cache_inputs(lens, fresh, prefix, page, heads, dtype, seed, poison=None, spare=3, extra=0):

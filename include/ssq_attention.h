@@ -126,7 +126,8 @@ int ssq_qk_norm_rope_f32(const float* q, int64_t q_stride, const float* k, int64
  * for token i of a sequence and query head h of key/value head h / group,
  *   out_i = sum_{j <= i} w_j v_j,   w = softmax_j(scale q_i . k_j),   j in the same sequence.
  * Scores, maxima, sums and outputs are held in binary32; the weights are rounded to bf16
- * for the product with v (as the values are), relative to a running maximum.
+ * for the product with v (as the values are), relative to a running maximum, and divided by
+ * the sum of the rounded ones.
  *
  *   starts    device, int32 [requests + 1], ascending from 0: sequence r holds the
  *             tokens starts[r] ... starts[r + 1] - 1 (none is valid); values are clamped to

@@ -5,6 +5,8 @@
 // token moves, so what bounds it is latency: one launch, in which every workgroup forms the
 // sums for itself (1024 requests at a time, in LDS) instead of waiting for another's, then
 // takes its share of the tokens and of the new pages and finds their requests by bisection.
+// 64 requests of one token: 3.7 us of graph time, a launch by itself 2.7; 256 prompts of up to
+// 2048 tokens: 8 us.
 #include "attention_internal.h"
 
 namespace ssq {

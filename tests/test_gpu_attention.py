@@ -313,6 +313,19 @@ MANY = [
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("prefix", [0, 70])
+@pytest.mark.parametrize("n", [64, 65, 131])
+def test_decode_requests_of_all_lengths(n, prefix, dtype):
+    """More requests than places, so that they are taken longest first: empty, equal and long ones."""
+    some = [0, 700, 33, 700, 1, 64, 699, 5, 128, 0, 300]
+    lens = [0 if some[r % 11] == 0 else prefix + some[r % 11] - r % 3 * (some[r % 11] > 9) for r in range(n)]
+    heads = (18, 9, 64)
+    q, k, v, table, _ = cache_inputs(lens, 1, prefix, 64, heads, dtype, 120 + n, poison=float("nan"))
+    ref, size, eps = A.decode_reference(q, k, v, table, lens, max(lens), prefix)
+    A.check(run_decode(q, k, v, table, lens, prefix), ref, size, eps, f"{n} {prefix} {dtype}")
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("i", range(len(MANY)))
 def test_decode_many_rows_behind_a_prefix(i, dtype):
     lens, fresh, prefix, page, heads = MANY[i]

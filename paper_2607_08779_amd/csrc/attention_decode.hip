@@ -8,16 +8,16 @@
 //   of the shared prefix, 64 keys at a time through two stages of LDS that the four
 //   wavefronts share.
 // * narrow: up to 32 query rows (one request's; or all requests', against the prefix, where they
-//   are no more than 32 in all, and in binary32) against a stretch of keys that the four wavefronts take 32 at a time, each through
-//   LDS of its own and without barriers: the next keys are loaded as soon as the scores of
-//   these are formed, the next values after the product.  Rows beside the used ones
-//   cost nothing that is scarce here.
+//   are no more than 32 in all, and in binary32) against a stretch of keys that the four
+//   wavefronts take 32 at a time, each through LDS of its own and without barriers: the next
+//   keys are loaded as soon as the scores of these are formed, the next values after the
+//   product.  Rows beside the used ones cost nothing that is scarce here.
 //
 // Bound by memory where the keys are the requests' own: one user's 16383 tokens (8 heads of 128)
 // take 18 us, of which 9.7 are the walk over the keys at 6.9 TB/s, the rest the start, the end and
 // the launch that joins.  64 users behind a shared prefix of 8192 tokens, 1 to 1024 of their own,
-// take 42 us where the cache lies partly in the Infinity Cache and 52 where it does not (175 MB,
-// 3.3 TB/s): workgroups of 2 to 20 us of work on 512 places end unevenly.
+// take 42 us where the cache lies partly in the Infinity Cache and 49 where it does not (175 MB,
+// 3.6 TB/s): workgroups of 2 to 20 us of work on 512 places end unevenly.
 //
 // Parts leave O unnormalised in binary32 with its reference and sum, and are joined as
 //   out = sum_s 2^(m_s - M) O_s / sum_s 2^(m_s - M) l_s,   M = max_s m_s.

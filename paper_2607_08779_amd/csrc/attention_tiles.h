@@ -441,26 +441,19 @@ struct Rows32 {
     return !(z == 0.0f);
   }
 
-  // Outputs times `by` to the row at `out`.  In bf16 lane and lane ^ 32 exchange halves so that
-  // each stores 16 bytes.
-  __device__ __forceinline__ void store(T* out, bool present, float by, int lane) const {
+  // Outputs times `by` to the row at `out`, in bf16: lane and lane ^ 32 exchange halves so that each
+  // stores 16 bytes.
+  __device__ __forceinline__ void store(uint16_t* out, bool present, float by, int lane) const {
 #pragma unroll
-    for (int t = 0; t < S::kOut; ++t) {
-      if constexpr (sizeof(T) == 2) {
+    for (int t = 0; t < S::kOut; ++t)
 #pragma unroll
-        for (int a = 0; a < 4; a += 2) {
-          const auto x = __builtin_amdgcn_permlane32_swap(pack_bf16x2(o[t][4 * a] * by, o[t][4 * a + 1] * by),
-                                                          pack_bf16x2(o[t][4 * a + 4] * by, o[t][4 * a + 5] * by), false, false);
-          const auto y = __builtin_amdgcn_permlane32_swap(pack_bf16x2(o[t][4 * a + 2] * by, o[t][4 * a + 3] * by),
-                                                          pack_bf16x2(o[t][4 * a + 6] * by, o[t][4 * a + 7] * by), false, false);
-          if (present) *reinterpret_cast<u32x4*>(out + 32 * t + 8 * a + 8 * (lane / 32)) = u32x4{x[0], y[0], x[1], y[1]};
-        }
-      } else if (present) {
-#pragma unroll
-        for (int a = 0; a < 4; ++a)
-          *reinterpret_cast<f32x4*>(out + 32 * t + 8 * a + 4 * (lane / 32)) = f32x4{o[t][4 * a] * by, o[t][4 * a + 1] * by, o[t][4 * a + 2] * by, o[t][4 * a + 3] * by};
+      for (int a = 0; a < 4; a += 2) {
+        const auto x = __builtin_amdgcn_permlane32_swap(pack_bf16x2(o[t][4 * a] * by, o[t][4 * a + 1] * by),
+                                                        pack_bf16x2(o[t][4 * a + 4] * by, o[t][4 * a + 5] * by), false, false);
+        const auto y = __builtin_amdgcn_permlane32_swap(pack_bf16x2(o[t][4 * a + 2] * by, o[t][4 * a + 3] * by),
+                                                        pack_bf16x2(o[t][4 * a + 6] * by, o[t][4 * a + 7] * by), false, false);
+        if (present) *reinterpret_cast<u32x4*>(out + 32 * t + 8 * a + 8 * (lane / 32)) = u32x4{x[0], y[0], x[1], y[1]};
       }
-    }
   }
 };
 

@@ -92,8 +92,16 @@ Plan make_plan(int64_t requests, int fresh, int q_heads, int kv_heads, int64_t m
   } else {
     prefix = 0;
   }
-  p.own_parts = (int)std::clamp(ceil_div(kGroups, requests * kv_heads * p.own_tiles), (int64_t)1,
-                                std::min<int64_t>(kMaxParts / 2, std::max<int64_t>(1, ceil_div(max_len - prefix, 256))));
+  // Fewest keys of a part of a request's own, of which a workgroup takes 128 in about a us.  Beside a
+  // prefix 768: its parts take that long, and are joined in any case (30 requests of up to 300 keys
+  // behind 300: 14.0 us a step, 16.7 with parts of 256).  Else one part up to 384 keys, whose join
+  // would take longer (300 keys: 8.0 us, 9.4 in two parts); then 128 where the parts have a CU
+  // each (900 keys: 8.4, 9.4 with 256), and 256 where they do not (4 requests of 2048: 12.7, 13.8
+  // with 128).
+  const int64_t behind = max_len - prefix, groups = requests * kv_heads * p.own_tiles;
+  const int64_t fewest = p.share != kShareNone ? 768 : behind <= 384 ? 384 : groups * ceil_div(behind, kNarrowKeys) <= 256 ? kNarrowKeys : 256;
+  p.own_parts = (int)std::clamp(ceil_div(kGroups, groups), (int64_t)1,
+                                std::min<int64_t>(kMaxParts / 2, std::max<int64_t>(1, ceil_div(behind, fewest))));
   return p;
 }
 

@@ -10,10 +10,12 @@
 // order of a sum's terms is free): slots 0-3 of a lane are keys 4 h + (0..3), slots 4-7
 // keys 8 + 4 h + (0..3).  V^T is read from row-major V in LDS by transposing reads in that order.
 //
-// O and the sum of the weights are relative to a running reference m (log2 units): weights
-// are 2^(scale log2(e) s - m).  m only moves, and O is only rescaled, when a tile's maximum
-// exceeds it by more than kSlack: weights stay below 2^kSlack, far from any overflow, and
-// their relative rounding to bf16 does not depend on m.
+// O and the sum of the weights are relative to a running reference m (log2 units) of each row:
+// weights are 2^(scale log2(e) s - m).  m only moves, and O is only rescaled, when a tile's
+// maximum of that row exceeds it by more than kSlack: weights stay at or below 2^kSlack, far from any
+// overflow.  In bf16 the weights are rounded to 8 significant bits for the product, because the
+// matrix cores take both operands in one type; each is off by up to 2^-9 of itself, whatever m is,
+// though by how much depends on m's fraction.
 //
 // Both tiles live in LDS as rows of D elements, 16-byte chunks XOR-swizzled so that the 16 lanes
 // an access serves at once spread over all banks; the swizzle is applied to the global address
@@ -365,8 +367,9 @@ struct Rows32 {
       }
   }
 
-  // Moves the reference where a score of these exceeds it by more than kSlack.  A NaN score leaves
-  // it as it is and spoils its row by its weight.
+  // Moves a row's reference where a score of its own exceeds it by more than kSlack, and no other
+  // row's: weights are rounded relative to it, so what shares the tile would show in the result.
+  // A NaN score leaves it as it is and spoils its row by its weight.
   template <int KT>
   __device__ __forceinline__ void raise(const f32x16 (&s)[KT], float scale) {
     float top = s[0][0];
@@ -376,7 +379,7 @@ struct Rows32 {
       for (int i = 0; i < 16; ++i) top = __builtin_elementwise_maximum(top, s[kt][i]);
     top = max_across(top) * scale;
     if (__builtin_expect(__builtin_amdgcn_ballot_w64(top > m + kSlack) != 0, 0)) {
-      const float to = fmaxf(m, top), by = __builtin_amdgcn_exp2f(m - to);
+      const float to = top > m + kSlack ? top : m, by = __builtin_amdgcn_exp2f(m - to);
       m = to;
       l *= by;
 #pragma unroll

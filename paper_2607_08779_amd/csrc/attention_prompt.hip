@@ -128,7 +128,7 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(const Prompt<T> a, 
   if (threadIdx.x == 0) spoiled = 0;
   walk(std::false_type{});
   // An infinite or NaN value can have reached rows of its tile that do not see it: then once
-  // more, edge tiles key by key.
+  // more, in edge tiles such values apart and key by key.
   if (present && r.spoiled()) spoiled = 1;
   __syncthreads();
   if (spoiled != 0) walk(std::true_type{});

@@ -61,6 +61,8 @@ __device__ __forceinline__ int value_swizzle(int row) {
   return sizeof(T) == 4 ? 0 : D == 128 ? 4 * (row & 3) : 4 * ((row >> 1) & 1);
 }
 
+__device__ __forceinline__ bool is_finite(float v) { return (__float_as_uint(v) & 0x7f800000u) != 0x7f800000u; }
+
 __device__ __forceinline__ float max_across(float v) {       // of lane and lane ^ 32
   const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
   return fmaxf(__uint_as_float(s[0]), __uint_as_float(s[1]));
@@ -215,13 +217,23 @@ struct Products<uint16_t, D> {
     const auto lo = __builtin_bit_cast(u32x2, d[0]), hi = __builtin_bit_cast(u32x2, d[1]);
     return __builtin_bit_cast(bf16x8, u32x4{lo.x, lo.y, hi.x, hi.y});
   }
-  template <int KT>
+  // The same with zeros for infinities and NaN.
+  static __device__ __forceinline__ bf16x8 finite(bf16x8 v) {
+    u32x4 d = __builtin_bit_cast(u32x4, v);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      d[i] &= ((d[i] & 0x7f80u) == 0x7f80u ? 0u : 0xffffu) | ((d[i] & 0x7f800000u) == 0x7f800000u ? 0u : 0xffff0000u);
+    return __builtin_bit_cast(bf16x8, d);
+  }
+  template <bool FINITE, int KT>
   __device__ __forceinline__ void accumulate(const uint8_t* values, const Weights<KT>& p, f32x16 (&o)[S::kOut]) const {
 #pragma unroll
     for (int c = 0; c < 2 * KT; ++c)
 #pragma unroll
-      for (int t = 0; t < S::kOut; ++t)
-        o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(value(values, c, t), __builtin_bit_cast(bf16x8, p.w[c]), o[t], 0, 0, 0);
+      for (int t = 0; t < S::kOut; ++t) {
+        const bf16x8 v = value(values, c, t);
+        o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(FINITE ? finite(v) : v, __builtin_bit_cast(bf16x8, p.w[c]), o[t], 0, 0, 0);
+      }
   }
   // One key's weight for this lane's column, and four of its values.
   template <int KT>
@@ -284,16 +296,17 @@ struct Products<float, D> {
   static __device__ __forceinline__ float add_weights(const Weights<KT>& p, int kt, int i, float sum) {
     return sum + (p.w[kt][2 * i] + p.w[kt][2 * i + 1]);
   }
-  template <int KT>
+  template <bool FINITE, int KT>
   __device__ __forceinline__ void accumulate(const uint8_t* values, const Weights<KT>& p, f32x16 (&o)[S::kOut]) const {
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
       for (int i = 0; i < 16; ++i)
 #pragma unroll
-        for (int t = 0; t < S::kOut; ++t)
-          o[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(*reinterpret_cast<const float*>(values + v_base + (32 * kt + 8 * (i / 4) + i % 4) * S::kRow + 128 * t),
-                                                      p.w[kt][i], o[t], 0, 0, 0);
+        for (int t = 0; t < S::kOut; ++t) {
+          const float v = *reinterpret_cast<const float*>(values + v_base + (32 * kt + 8 * (i / 4) + i % 4) * S::kRow + 128 * t);
+          o[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(FINITE && !is_finite(v) ? 0.0f : v, p.w[kt][i], o[t], 0, 0, 0);
+        }
   }
   template <int KT>
   static __device__ __forceinline__ float weight_of(const Weights<KT>& p, int key) {
@@ -407,11 +420,12 @@ struct Rows32 {
     l += sum[0] + sum[1];
   }
 
-  // The product with the values key by key, adding only to the rows that see the key: a weight
-  // of zero times an infinite or NaN value of a hidden key is NaN, and the matrix cores add
-  // such products to every row of a tile.
+  // What values that are infinite or NaN add, key by key and only to the rows that see the key: a
+  // weight of zero times such a value of a hidden key is NaN, and the matrix cores add the product
+  // to every row of a tile.  The finite ones stay with the matrix cores, so that a row's bits are
+  // the same whatever is hidden from it.
   template <int KT>
-  __device__ __forceinline__ void accumulate_careful(const uint8_t* values, const typename P::template Weights<KT>& p, int last, int lane) {
+  __device__ __forceinline__ void accumulate_others(const uint8_t* values, const typename P::template Weights<KT>& p, int last, int lane) {
 #pragma unroll 1
     for (int key = 0; key < 32 * KT; ++key) {
       const float w = P::weight_of(p, key);
@@ -421,7 +435,7 @@ struct Rows32 {
         for (int a = 0; a < 4; ++a) {
           const f32x4 v = P::values_of(values, key, 32 * t + 8 * a + 4 * (lane / 32));
 #pragma unroll
-          for (int e = 0; e < 4; ++e) o[t][4 * a + e] = key <= last ? __builtin_fmaf(w, v[e], o[t][4 * a + e]) : o[t][4 * a + e];
+          for (int e = 0; e < 4; ++e) o[t][4 * a + e] = key <= last && !is_finite(v[e]) ? __builtin_fmaf(w, v[e], o[t][4 * a + e]) : o[t][4 * a + e];
         }
     }
   }
@@ -429,9 +443,12 @@ struct Rows32 {
   template <bool CAREFUL, int KT>
   __device__ __forceinline__ void add(const uint8_t* values, const typename P::template Weights<KT>& p, bool edge, int last, int lane) {
     if constexpr (CAREFUL) {
-      if (edge) return accumulate_careful<KT>(values, p, last, lane);
+      if (edge) {
+        x.template accumulate<true, KT>(values, p, o);
+        return accumulate_others<KT>(values, p, last, lane);
+      }
     }
-    x.template accumulate<KT>(values, p, o);
+    x.template accumulate<false, KT>(values, p, o);
   }
 
   // Whether an output of this lane's row is not finite.

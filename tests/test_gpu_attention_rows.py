@@ -84,3 +84,68 @@ def test_decode_draft_does_not_depend_on_later_ones(prefix, dtype):
         q2[:, 3:] = sharp(A.model_like(gen(290), (3, 2, heads[0], heads[2]), dtype), times)
         again = run_decode(q2, k2, v2, table, lens, prefix)
         check_bits(again[:, :3], out[:, :3], f"times {times}")
+
+
+# Hidden keys and values of any bits: those that are no numbers, and the largest that are
+BAD = [float("nan"), float("inf"), -float("inf"), 3e38]
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("bad", BAD)
+@pytest.mark.parametrize("i", range(len(PROMPTS)))
+def test_prompt_hidden_keys_of_any_bits_change_none(i, bad, dtype):
+    lens, heads, p = PROMPTS[i]
+    q, k, v = prompt_inputs(lens, heads, dtype, 310 + i)
+    starts = ints(A.starts_of(lens))
+    out = ssq.ssq_attention_prompt(sharp(q, 2.0), k, v, starts)
+    for step in (1, 3):
+        k2, v2 = k.clone(), v.clone()
+        k2[p::step, :, ::3] = bad
+        v2[p::step, :, 1::2] = bad
+        check_bits(ssq.ssq_attention_prompt(sharp(q, 2.0), k2, v2, starts)[:p], out[:p], f"{lens} {heads} {bad} {step}")
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("bad", BAD)
+@pytest.mark.parametrize("prefix", [0, 64, 100])
+def test_decode_hidden_keys_of_any_bits_change_none(prefix, bad, dtype):
+    """A late draft of one request, what another holds behind the prefix, and what no request holds; requests that
+    end inside the prefix see less of it than others."""
+    fresh, page, heads = 5, 16, (16, 2, 128)
+    lens = [130, 97, 200] + [101 + i for i in range(20)]
+    q, k, v, table, _ = cache_inputs(lens, fresh, prefix, page, heads, dtype, 330)
+    out = run_decode(sharp(q, 2.0), k, v, table, lens, prefix)
+    k2, v2 = k.clone(), v.clone()
+    e, t = int(table[0, 128 // page]), 128 % page           # request 0: the fourth draft of five
+    k2[e, :, t, ::3], v2[e, :, t, 1::2] = bad, bad
+    for r, n in enumerate(lens):                            # past every request's end
+        at = n % page
+        if at:
+            k2[int(table[r, n // page]), :, at:], v2[int(table[r, n // page]), :, at:] = bad, bad
+    got = run_decode(sharp(q, 2.0), k2, v2, table, lens, prefix)
+    check_bits(got[1:], out[1:], f"{bad}")
+    check_bits(got[0, :3], out[0, :3], f"{bad} drafts")
+    short = [60, 97] + lens[2:]
+    if prefix:                                              # the prefix's later keys, which request 0 does not see
+        first = run_decode(sharp(q, 2.0), k, v, table, short, prefix)
+        for t in range(60, prefix):
+            k2[int(table[0, t // page]), :, t % page, ::3] = bad
+            v2[int(table[0, t // page]), :, t % page, 1::2] = bad
+        check_bits(run_decode(sharp(q, 2.0), k2, v2, table, short, prefix)[0], first[0], f"{bad} short")
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("lens,heads", [([150, 60], (8, 2, 64)), ([400], (4, 1, 128))])
+def test_prompt_values_that_are_no_numbers_reach_exactly_the_rows_that_see_them(lens, heads, dtype):
+    q, k, v = prompt_inputs(lens, heads, dtype, 350)
+    starts, (hq, hk, d) = ints(A.starts_of(lens)), heads
+    out = ssq.ssq_attention_prompt(q, k, v, starts)
+    v2 = v.clone()
+    v2[37, 0, 5], v2[100, 0, 6], v2[70, 0, 5] = float("inf"), float("nan"), -float("inf")
+    got = ssq.ssq_attention_prompt(q, k, v2, starts).float()
+    end, g = lens[0], hq // hk
+    assert (got[37:70, :g, 5] == float("inf")).all() and torch.isnan(got[70:end, :g, 5]).all() and torch.isnan(got[100:end, :g, 6]).all()
+    want = out.float()
+    for a, c in ((37, 5), (100, 6)):
+        got[a:end, :g, c] = want[a:end, :g, c] = 0
+    check_bits(got, want, "the others")

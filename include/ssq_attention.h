@@ -30,7 +30,8 @@
  *     slots and positions outside their range are handled as each entry point says, and
  *     never cause an access outside the arrays that were passed.
  *   - Keys that a query does not see have no influence on its result, whatever their
- *     bits (infinities and NaN included).  A query that sees no key gives zeros.
+ *     bits (infinities and NaN included): it is the same to the last bit.  A query that
+ *     sees no key gives zeros; one whose scores are all -infinity gives NaN.
  */
 #ifndef SSQ_ATTENTION_H
 #define SSQ_ATTENTION_H

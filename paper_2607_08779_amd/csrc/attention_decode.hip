@@ -155,7 +155,7 @@ template <typename T, int D>
 __device__ __forceinline__ void put(const Decode<T>& a, const Plan& p, const Parts& parts, int part, const Row& row,
                                     int at, f32x4 o, float m, float l) {
   if (parts.ml == nullptr) {
-    const float by = l != 0.0f ? 1.0f / l : 0.0f;
+    const float by = inverse_of(l);
     T* to = a.out.p + row.line * a.out.stride + row.column * D + at;
     if constexpr (sizeof(T) == 2) *reinterpret_cast<u32x2*>(to) = u32x2{pack_bf16x2(o[0] * by, o[1] * by), pack_bf16x2(o[2] * by, o[3] * by)};
     else *reinterpret_cast<f32x4*>(to) = f32x4{o[0] * by, o[1] * by, o[2] * by, o[3] * by};
@@ -210,7 +210,7 @@ __device__ void wide(const Decode<T>& a, const Plan& p, const Parts& parts, int 
         [&](uint8_t* to) { load.keys(describe(a.cache.k + at, bytes), to + wave * S::kGroup); },
         [&](uint8_t* to) { load.values(describe(a.cache.v + at, bytes), to + wave * S::kGroup); },
         [&](int t) { return begin + kWideKeys * (t + 1) - 1 > min(wave_first, end - 1) || absent != 0; },
-        [&](int t, f32x16 (&s)[2]) { Rows32<T, D>::template mask<2>(s, 0, min(row.last, end - 1) - begin - kWideKeys * t, absent, lane); },
+        [&](int t, f32x16 (&s)[2]) { return Rows32<T, D>::template mask<2>(s, 0, min(row.last, end - 1) - begin - kWideKeys * t, absent, lane); },
         [&](int t) { return min(row.last, end - 1) - begin - kWideKeys * t; });
   };
   if (threadIdx.x == 0) *spoiled = 0;
@@ -351,10 +351,11 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const Decode<T> a, int64
     o[i] = s < count ? *reinterpret_cast<const f32x4*>(from + s * line_rows * D) : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   }
   // every wavefront forms the parts' weights, for itself
-  const float2 x = lane < count ? parts.ml[lane * line_rows + row] : float2{-FLT_MAX, 0.0f};
+  const float2 x = lane < count ? parts.ml[lane * line_rows + row] : float2{-FLT_MAX, __uint_as_float(kSawNone)};
   const float m = wave_max(x.y != 0.0f ? x.x : -FLT_MAX);
   const float by = x.y != 0.0f ? __builtin_amdgcn_exp2f(x.x - m) : 0.0f;
-  const float l = wave_sum(by * x.y);
+  float l = wave_sum(by * x.y);
+  if (l == 0.0f && __builtin_amdgcn_ballot_w64(__float_as_uint(x.y) != kSawNone) == 0) l = __uint_as_float(kSawNone);
   f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
   for (int i = 0; i < kMaxParts / kGroups; ++i) {

@@ -122,7 +122,7 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(const Prompt<T> a, 
           v_at += kTileKeys;
         },
         [&](int t) { return kTileKeys * t + kTileKeys - 1 > wave_first; },
-        [&](int t, f32x16 (&s)[2]) { Rows32<T, D>::template mask<2>(s, 0, last - kTileKeys * t, 0u, lane); },
+        [&](int t, f32x16 (&s)[2]) { return Rows32<T, D>::template mask<2>(s, 0, last - kTileKeys * t, 0u, lane); },
         [&](int t) { return last - kTileKeys * t; });
   };
   if (threadIdx.x == 0) spoiled = 0;
@@ -132,8 +132,7 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(const Prompt<T> a, 
   if (present && r.spoiled()) spoiled = 1;
   __syncthreads();
   if (spoiled != 0) walk(std::true_type{});
-  const float l = sum_across(r.l);
-  r.store(a.out.p + line * a.out.stride + column, present, l != 0.0f ? 1.0f / l : 0.0f, lane);
+  r.store(a.out.p + line * a.out.stride + column, present, inverse_of(sum_across(r.l)), lane);
 }
 
 // 32 rows a workgroup, whose wavefronts share out the keys.
@@ -167,7 +166,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void prompt_small
   walk(std::false_type{});
   if (__builtin_amdgcn_ballot_w64(present && r.spoiled()) != 0) walk(std::true_type{});
   join_waves<kWaves>(r, lds, ml, min(rows - row0, 32), wave, lane, [&](int of, int d, f32x4 o, float, float l) {
-    const float by = l != 0.0f ? 1.0f / l : 0.0f;
+    const float by = inverse_of(l);
     const int index = row0 + of, t = index / group;
     T* to = a.out.p + (at.begin + t) * a.out.stride + (head * group + index - t * group) * D + d;
     if constexpr (sizeof(T) == 2) *reinterpret_cast<u32x2*>(to) = u32x2{pack_bf16x2(o[0] * by, o[1] * by), pack_bf16x2(o[2] * by, o[3] * by)};

@@ -17,6 +17,10 @@
 // matrix cores take both operands in one type; each is off by up to 2^-9 of itself, whatever m is,
 // though by how much depends on m's fraction.
 //
+// The sum starts at -0 and leaves it with the first tile of which the row sees a key.  So a sum of -0
+// is that of a row that saw none, which gives zeros, and +0 that of one whose scores were all -inf,
+// which gives NaN as their softmax does (inverse_of).
+//
 // Both tiles live in LDS as rows of D elements, 16-byte chunks XOR-swizzled so that the 16 lanes
 // an access serves at once spread over all banks; the swizzle is applied to the global address
 // of a direct-to-LDS load, whose LDS side is linear.
@@ -71,6 +75,11 @@ __device__ __forceinline__ float sum_across(float v) {
   const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
   return __uint_as_float(s[0]) + __uint_as_float(s[1]);
 }
+
+constexpr uint32_t kSawNone = 0x80000000u;      // the bits of -0
+
+// What the outputs are multiplied by for the sum l of a row's weights.
+__device__ __forceinline__ float inverse_of(float l) { return __float_as_uint(l) == kSawNone ? 0.0f : 1.0f / l; }
 
 // A reduction over the wavefront's 64 lanes in six DPP moves (shifts within rows of 16 lanes, then
 // broadcasts across them), an eighth of the latency of as many exchanges through LDS; lanes that a
@@ -340,7 +349,7 @@ struct Rows32 {
 #pragma unroll
       for (int i = 0; i < 16; ++i) o[t][i] = 0.0f;
     m = -FLT_MAX;
-    l = 0.0f;
+    l = __uint_as_float(kSawNone);
   }
 
   // S^T of 32 KT keys: the tiles in turn, each piece of the keys read four products ahead.
@@ -366,10 +375,11 @@ struct Rows32 {
   }
 
   // Scores of keys outside [first, last], counted from the tile's first key, and of absent
-  // groups of 16 (bits of `absent`) become those of keys that are not seen.
+  // groups of 16 (bits of `absent`) become those of keys that are not seen; true if one is.
   template <int KT>
-  static __device__ __forceinline__ void mask(f32x16 (&s)[KT], int first, int last, uint32_t absent, int lane) {
+  static __device__ __forceinline__ bool mask(f32x16 (&s)[KT], int first, int last, uint32_t absent, int lane) {
     const int h4 = 4 * (lane / 32);
+    bool seen = false;
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
@@ -377,7 +387,9 @@ struct Rows32 {
         const int key = 32 * kt + 8 * (i / 4) + i % 4 + h4;
         const bool hidden = (key < first) | (key > last) | ((absent >> (2 * kt + i / 8) & 1u) != 0);
         s[kt][i] = hidden ? -__builtin_inff() : s[kt][i];
+        seen |= !hidden;
       }
+    return seen;
   }
 
   // Moves a row's reference where a score of its own exceeds it by more than kSlack, and no other
@@ -402,11 +414,11 @@ struct Rows32 {
     }
   }
 
-  // Weights of 32 KT keys from their scores, and the running sum.  The sum is that of the weights as
+  // Weights of 32 KT keys, one of which the row sees or none, from their scores, and the running sum.  The sum is that of the weights as
   // the product takes them, so that their rounding is one of weights that still add up to one
   // (in bf16: a row of one or a few keys comes out as exact as its values are).
   template <int KT>
-  __device__ __forceinline__ void weights(const f32x16 (&s)[KT], float scale, typename P::template Weights<KT>& p) {
+  __device__ __forceinline__ void weights(const f32x16 (&s)[KT], float scale, bool seen, typename P::template Weights<KT>& p) {
     float sum[2] = {0.0f, 0.0f};
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt)
@@ -417,7 +429,7 @@ struct Rows32 {
         P::set(p, kt, i, a, b);
         sum[i % 2] = P::add_weights(p, kt, i, sum[i % 2]);
       }
-    l += sum[0] + sum[1];
+    l = seen ? l + (sum[0] + sum[1]) : l;
   }
 
   // What values that are infinite or NaN add, key by key and only to the rows that see the key: a
@@ -482,8 +494,8 @@ struct Rows32 {
 // loads of tile t need, before the wait for those of tile t - 1, `keys(buffer)` and
 // `values(buffer)` load this wavefront's quarter of the next 64, in order; `tiles` are walked by
 // all, the first `mine` of them matter to this wavefront's rows; `edge(t)` says whether some row
-// does not see all keys of tile t, `hide(t, s)` then masks its scores, and `last(t)` is the last
-// key of tile t that the lane's row sees.
+// does not see all keys of tile t, `hide(t, s)` then masks its scores and says whether the lane's
+// row sees one, and `last(t)` is the last key of tile t that it sees.
 template <bool CAREFUL, typename T, int D, typename Ahead, typename Keys, typename Values, typename Edge, typename Hide, typename Last>
 __device__ __forceinline__ void walk_shared(Rows32<T, D>& r, uint8_t* lds, int tiles, int mine, float scale, int lane, Ahead ahead,
                                             Keys keys, Values values, Edge edge, Hide hide, Last last) {
@@ -504,10 +516,11 @@ __device__ __forceinline__ void walk_shared(Rows32<T, D>& r, uint8_t* lds, int t
     f32x16 s[2];
     r.scores(now, s);
     const bool hidden = edge(t);
-    if (__builtin_expect(hidden, 0)) hide(t, s);
+    bool seen = true;
+    if (__builtin_expect(hidden, 0)) seen = hide(t, s);
     r.template raise<2>(s, scale);
     typename Products<T, D>::template Weights<2> p;
-    r.template weights<2>(s, scale, p);
+    r.template weights<2>(s, scale, seen, p);
     r.template add<CAREFUL, 2>(now + kTile, p, CAREFUL && hidden, CAREFUL ? last(t) : 0, lane);
   };
   uint8_t *const a = lds, *const b = lds + 2 * kTile;
@@ -560,10 +573,11 @@ __device__ __forceinline__ void walk_private(Rows32<T, D>& r, uint8_t* lds, cons
     have_read();
 #pragma unroll
     for (int g = 0; g < 2; ++g) load_k.keys(describe(next[g].k, next[g].k_bytes), k + g * S::kGroup);
-    if (edge) Rows32<T, D>::template mask<1>(s, lo - j, min(last, hi - 1) - j, absent, lane);
+    bool seen = true;
+    if (edge) seen = Rows32<T, D>::template mask<1>(s, lo - j, min(last, hi - 1) - j, absent, lane);
     r.template raise<1>(s, scale);
     typename Products<T, D>::template Weights<1> p;
-    r.template weights<1>(s, scale, p);
+    r.template weights<1>(s, scale, seen, p);
     landed<2 * S::kLoads>();
     r.template add<CAREFUL, 1>(v, p, edge, min(last, hi - 1) - j, lane);
     have_read();
@@ -595,14 +609,17 @@ __device__ __forceinline__ void join_waves(const Rows32<T, D>& r, uint8_t* lds, 
   __syncthreads();
   for (int i = threadIdx.x; i < count * kPieces; i += 64 * WAVES) {
     const int at = i % kPieces, of = i / kPieces;
-    float m = ml[of].x, sum = 0.0f;
+    float m = ml[of].x, sum = __uint_as_float(kSawNone);
 #pragma unroll
     for (int w = 1; w < WAVES; ++w) m = fmaxf(m, ml[w * 32 + of].x);
     f32x4 all = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int w = 0; w < WAVES; ++w) {
       const float2 x = ml[w * 32 + of];
-      if (x.y == 0.0f) continue;
+      if (x.y == 0.0f) {
+        sum += x.y;                       // for its sign
+        continue;
+      }
       const float by = __builtin_amdgcn_exp2f(x.x - m);
       const f32x4 y = o[(w * 32 + of) * kPieces + (at ^ (of % kPieces))];
       sum = __builtin_fmaf(by, x.y, sum);

@@ -149,3 +149,58 @@ def test_prompt_values_that_are_no_numbers_reach_exactly_the_rows_that_see_them(
     for a, c in ((37, 5), (100, 6)):
         got[a:end, :g, c] = want[a:end, :g, c] = 0
     check_bits(got, want, "the others")
+
+
+# --- scores of minus infinity -------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("lens,heads", [([5], (4, 2, 64)), ([150, 60], (32, 8, 128)), ([400], (4, 1, 128)), ([130, 2], (8, 8, 64))])
+def test_prompt_rows_whose_scores_are_all_minus_infinity_are_nan(lens, heads, dtype):
+    """Softmax over scores of -inf alone has no value; beside any finite score their weight is zero."""
+    q, k, v = prompt_inputs(lens, heads, dtype, 400)
+    q[..., 0] = 1 + q[..., 0].abs()
+    starts = ints(A.starts_of(lens))
+    first = min(lens[0] - 1, 67)
+    k[:first, :, 0] = -float("inf")                          # every key of the first sequence before `first`
+    out = ssq.ssq_attention_prompt(q, k, v, starts)
+    assert torch.isnan(out[:first]).all()
+    a, b = first, lens[0]
+    A.check(out[a:b], *A.prompt_reference(q[a:b], k[a:b], v[a:b], [b - a]), "rows that see finite scores too")
+    if len(lens) > 1:
+        A.check(out[b:], *A.prompt_reference(q[b:], k[b:], v[b:], lens[1:]), "the other sequence")
+    k[..., 0] = -float("inf")
+    assert torch.isnan(ssq.ssq_attention_prompt(q, k, v, starts)).all()
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("prefix", [0, 64, 90])
+@pytest.mark.parametrize("n", [1, 3, 40])
+def test_decode_rows_whose_scores_are_all_minus_infinity_are_nan(n, prefix, dtype):
+    heads, page, fresh = (8, 2, 128), 16, 2
+    lens = [(1900, 131, 92)[r % 3] + r for r in range(n)]
+    q, k, v, table, _ = cache_inputs(lens, fresh, prefix, page, heads, dtype, 420 + n)
+    q[..., 0] = 1 + q[..., 0].abs()
+    bad = k.clone()
+    bad[..., 0] = -float("inf")
+    for ws in (None, torch.empty(0, dtype=torch.uint8, device="cuda")):
+        assert torch.isnan(run_decode(q, bad, v, table, lens, prefix, workspace=ws)).all()
+        # nothing seen is still nothing: no tokens, a token before the first, pages that are absent
+        assert not run_decode(q, bad, v, table, [0] * n, prefix, max_len=max(lens), workspace=ws).any()
+        one = run_decode(q, bad, v, table, [1] * n, prefix, max_len=max(lens), workspace=ws)
+        assert not one[:, 0].any() and torch.isnan(one[:, 1]).all()
+        assert not run_decode(q, bad, v, torch.full_like(table, -1), lens, prefix, workspace=ws).any()
+    # the first page is absent and the rest -inf; then only the last key of every request is finite
+    some = table.clone()
+    some[:, 0] = -1
+    assert torch.isnan(run_decode(q, bad, v, some, lens, prefix)).all()
+    for r, m in enumerate(lens):
+        bad[int(table[r, (m - 1) // page]), :, (m - 1) % page] = k[int(table[r, (m - 1) // page]), :, (m - 1) % page]
+    for ws in (None, torch.empty(0, dtype=torch.uint8, device="cuda")):
+        out = run_decode(q, bad, v, table, lens, prefix, workspace=ws)
+        assert torch.isnan(out[:, 0]).all()
+        for r, m in enumerate(lens):
+            want = v[int(table[r, (m - 1) // page]), :, (m - 1) % page].repeat_interleave(4, 0)
+            if dtype == BF:                                 # w v / w, to within binary32
+                check_bits(out[r, 1], want, f"the value of the one finite key, request {r}")
+            assert ((out[r, 1] - want).abs() <= 2.0 ** -20 * want.abs()).all()

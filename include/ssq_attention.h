@@ -70,8 +70,10 @@ extern "C" {
  *   lens         device, int32 [requests], written
  *   positions    device, int32 [tokens], written
  *   slots        device, int32 [tokens], written
- *   taken_after  device, int32 [1], written: *taken plus all pages needed; may be
- *                `taken` itself only in a later call's argument, not in the same call's
+ *   taken_after  device, int32 [1], written: *taken plus all pages needed
+ * No array that is written (`table` among them) may overlap another argument's, which
+ * workgroups still read: the `lens` and *taken_after of one call are `held` and *taken of
+ * a later one, in buffers of their own, not in the same call's.
  * Pages past the end of the list get the entry -1 and their tokens the slot -1 (then
  * *taken_after > free_count); so do tokens past a row's table_stride pages, whose pages
  * are counted and not stored.  Sums are those of 32-bit two's complement: fewer than

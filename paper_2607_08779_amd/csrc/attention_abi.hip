@@ -23,6 +23,16 @@ bool valid_heads(int q_heads, int kv_heads) {
 }
 int shift_of(int page_size) { return __builtin_ctz((unsigned)page_size); }
 
+// An array of 4-byte elements, which may be empty.
+struct Span {
+  const void* p;
+  int64_t count;
+};
+bool overlap(const Span& a, const Span& b) {
+  const auto x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
+  return a.count > 0 && b.count > 0 && x < y + 4 * (uintptr_t)b.count && y < x + 4 * (uintptr_t)a.count;
+}
+
 // Rows of `heads` heads: a stride that holds them, in whole 16-byte pieces.
 template <typename T>
 bool valid_stride(int64_t stride, int heads, int head_dim) {
@@ -42,6 +52,14 @@ int check_page_tables(const int32_t* held, const int32_t* added, int64_t request
     return SSQ_EINVAL;
   for (const void* p : {held, added, free_pages, taken, table, starts, lens, positions, slots, taken_after})
     if (!aligned(p, 4)) return SSQ_EALIGN;
+  // Every workgroup reads the lengths, the free list and the rows while others write: an output over
+  // any of them, or over another output, is a race.
+  const Span arrays[] = {{table, requests * table_stride}, {starts, requests + 1}, {lens, requests}, {positions, tokens}, {slots, tokens},
+                         {taken_after, 1}, {held, requests}, {added, requests}, {free_pages, free_count}, {taken, taken != nullptr}};
+  constexpr int kWritten = 6, kArrays = sizeof(arrays) / sizeof(arrays[0]);
+  for (int i = 0; i < kWritten; ++i)
+    for (int j = i + 1; j < kArrays; ++j)
+      if (overlap(arrays[i], arrays[j])) return SSQ_EINVAL;
   return SSQ_OK;
 }
 

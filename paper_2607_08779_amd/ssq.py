@@ -412,7 +412,7 @@ def ssq_page_tables(held: torch.Tensor, added: torch.Tensor, free_pages: torch.T
     ``table`` (int32 [requests, pages]) is updated in place.  Returns (starts [requests + 1],
     lens [requests], positions [tokens], slots [tokens], taken after [1], table), all int32;
     ``tokens`` may exceed the sum of ``added`` (padding: position 0, slot -1).  ``out`` = the
-    first five reuses buffers."""
+    first five reuses buffers, which must not be those of another argument (``held`` for lens)."""
     if held.dim() != 1 or table.dim() != 2:
         raise ValueError("held must be [requests] and table [requests, pages]")
     n, width = table.shape

@@ -1,0 +1,29 @@
+"""How the attention operators may be called: buffers, layouts and sizes."""
+import pytest
+import torch
+
+from paper_2607_08779_amd import ssq
+from tests import attention_common as A
+from tests.test_gpu_attention import ints
+
+pytestmark = pytest.mark.gpu
+
+
+def test_page_tables_lengths_of_one_step_are_held_by_the_next():
+    """A serving loop in two sets of buffers, of more tokens than a workgroup takes; in one set it is refused."""
+    n, page, width = 1500, 16, 6
+    held, taken, table = [7 * i % 40 for i in range(n)], 0, [[-1] * width for _ in range(n)]
+    free = list(range(n * width))
+    dev, dev_free = ints(table), ints(free)
+    sets = [[torch.empty(k, dtype=torch.int32, device="cuda") for k in (n + 1, n, n, n, 1)] for _ in range(2)]
+    sets[1][1].copy_(ints(held))
+    sets[1][4].zero_()
+    for step in range(4):
+        before, now = sets[(step + 1) % 2], sets[step % 2]
+        got = ssq.ssq_page_tables(before[1], ints([1] * n), dev_free, dev, page, n, taken=before[4], out=now)
+        want = A.tables_reference(held, [1] * n, free, taken, page, table, n)
+        assert [x.tolist() if j != 4 else x.item() for j, x in enumerate(got)] == list(want)
+        held, taken, table = want[1], want[4], want[5]
+        for bad in ([*now[:1], before[1], *now[2:]], [before[1].new_empty(n + 1), now[1], now[1], *now[3:]]):
+            with pytest.raises(ssq.SSQError):
+                ssq.ssq_page_tables(before[1], ints([1] * n), dev_free, dev, page, n, taken=before[4], out=bad)

@@ -95,7 +95,7 @@ int ssq_page_tables(const int32_t* held, const int32_t* added, int64_t requests,
  *
  *   q, k, v         device, bf16; v is read only if a cache is given (else it may be NULL)
  *   *_stride        elements between two tokens' rows
- *   tokens          >= 0
+ *   tokens          >= 0; tokens * (q_heads + 2 kv_heads) * head_dim elements of at most 127 GiB
  *   q_gain, k_gain  device, bf16 [head_dim], or NULL: no norm for those heads
  *   eps             >= 0
  *   positions       device, int32 [tokens]
@@ -136,7 +136,7 @@ int ssq_qk_norm_rope_f32(const float* q, int64_t q_stride, const float* k, int64
  *             tokens starts[r] ... starts[r + 1] - 1 (none is valid); values are clamped to
  *             [0, tokens]; tokens from starts[requests] on are padding and give zeros
  *   requests  0 to 2^20
- *   tokens    rows of q, k, v and out; tokens * q_heads < 2^31
+ *   tokens    rows of q, k, v and out; tokens * q_heads + 128 (requests + 1) kv_heads < 2^31
  *   scale     finite, > 0 (1 / sqrt(head_dim) in these models)
  *   out       device, bf16, written; must not overlap q, k or v
  */
@@ -145,7 +145,8 @@ int ssq_attention_prompt(const uint16_t* q, int64_t q_stride, const uint16_t* k,
                          int64_t tokens, int q_heads, int kv_heads, int head_dim, float scale,
                          uint16_t* out, int64_t out_stride, hipStream_t stream);
 
-/* ssq_attention_prompt for binary32 q, k, v and out (weights in binary32 too). */
+/* ssq_attention_prompt for binary32 q, k, v and out (weights in binary32 too);
+ * tokens * q_heads + 32 (requests + 1) kv_heads < 2^29. */
 int ssq_attention_prompt_f32(const float* q, int64_t q_stride, const float* k, int64_t k_stride,
                              const float* v, int64_t v_stride, const int32_t* starts, int64_t requests,
                              int64_t tokens, int q_heads, int kv_heads, int head_dim, float scale,
@@ -168,7 +169,7 @@ int ssq_attention_prompt_f32(const float* q, int64_t q_stride, const float* k, i
  *
  *   q, out     device, bf16 [requests * fresh, q_heads, head_dim]: the tokens of request r
  *              are rows r * fresh ... r * fresh + fresh - 1; out must not overlap q
- *   requests   0 to 2^20;  fresh >= 1;  requests * fresh * q_heads < 2^31
+ *   requests   0 to 2^20;  fresh >= 1;  requests * (fresh * q_heads + 32 kv_heads) < 2^29
  *   lens       device, int32 [requests]: tokens in the cache, the new ones among them
  *   max_len    host bound of lens (it sizes the launch): 0 to 2^30
  *   prefix     >= 0

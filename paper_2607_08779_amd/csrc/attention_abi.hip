@@ -9,7 +9,8 @@
 namespace {
 
 constexpr int64_t kMaxRequests = int64_t(1) << 20;
-constexpr int64_t kMaxHeads = int64_t(1) << 31;      // tokens * heads (kernels index rows in int)
+constexpr int64_t kMaxRows = int64_t(1) << 31;       // kernels index rows in int
+constexpr int64_t kMaxRopeBytes = int64_t(127) << 30; // of all heads: 32 bytes a thread, of which a grid holds fewer than 2^32
 constexpr int64_t kMaxStride = int64_t(1) << 24;     // elements between rows (32-bit tile offsets)
 constexpr int64_t kMaxLen = int64_t(1) << 30;
 constexpr int kMaxHeadCount = 1 << 16;
@@ -71,7 +72,7 @@ int norm_rope(const T* q, int64_t q_stride, const T* k, int64_t k_stride, const 
   if (tokens < 0 || !valid_heads(q_heads, kv_heads) || !valid_dim(head_dim) || !(eps >= 0.0f) || !std::isfinite(eps) ||
       rope_rows < 0 || rope_rows > INT32_MAX)
     return SSQ_EINVAL;
-  if (tokens > kMaxLen || tokens * ((int64_t)q_heads + 2 * kv_heads) >= kMaxHeads) return SSQ_EINVAL;
+  if (tokens > kMaxLen || tokens * ((int64_t)q_heads + 2 * kv_heads) > kMaxRopeBytes / (head_dim * (int64_t)sizeof(T))) return SSQ_EINVAL;
   const bool cache = slots != nullptr;
   if (cache != (k_pages != nullptr) || cache != (v_pages != nullptr)) return SSQ_EINVAL;
   if (cache && (!valid_page(page_size) || pages < 0 || pages > INT32_MAX / page_size)) return SSQ_EINVAL;
@@ -101,7 +102,8 @@ int prompt(const T* q, int64_t q_stride, const T* k, int64_t k_stride, const T* 
   if (tokens < 0 || requests < 0 || requests > kMaxRequests || !valid_heads(q_heads, kv_heads) || !valid_dim(head_dim) ||
       !(scale > 0.0f) || !std::isfinite(scale))
     return SSQ_EINVAL;
-  if (tokens > kMaxLen || tokens * q_heads >= kMaxHeads || requests * q_heads >= kMaxHeads) return SSQ_EINVAL;
+  constexpr int64_t kRows = sizeof(T) == 2 ? 128 : 32;      // of a workgroup; where bf16 takes 32, it launches few
+  if (tokens > kMaxLen || tokens * q_heads + kRows * (requests + 1) * kv_heads >= kRows * ssq::kMaxGroups) return SSQ_EINVAL;
   if (!valid_stride<T>(q_stride, q_heads, head_dim) || !valid_stride<T>(out_stride, q_heads, head_dim) ||
       !valid_stride<T>(k_stride, kv_heads, head_dim) || !valid_stride<T>(v_stride, kv_heads, head_dim))
     return SSQ_EINVAL;
@@ -118,7 +120,8 @@ bool valid_decode_sizes(int64_t requests, int fresh, int q_heads, int kv_heads, 
   if (requests < 0 || requests > kMaxRequests || fresh < 1 || !valid_heads(q_heads, kv_heads) || !valid_dim(head_dim) ||
       max_len < 0 || max_len > kMaxLen || prefix < 0)
     return false;
-  return fresh <= kMaxLen && requests * fresh < kMaxHeads && requests * fresh * q_heads < kMaxHeads;
+  return fresh <= kMaxLen && requests * fresh < kMaxRows &&
+         requests * fresh * q_heads + 32 * requests * kv_heads < 32 * ssq::kMaxGroups;      // own rows, 32 a workgroup
 }
 
 template <typename T>

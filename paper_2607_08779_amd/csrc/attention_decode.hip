@@ -102,6 +102,9 @@ Plan make_plan(int64_t requests, int fresh, int q_heads, int kv_heads, int64_t m
   const int64_t fewest = p.share != kShareNone ? 768 : behind <= 384 ? 384 : groups * ceil_div(behind, kNarrowKeys) <= 256 ? kNarrowKeys : 256;
   p.own_parts = (int)std::clamp(ceil_div(kGroups, groups), (int64_t)1,
                                 std::min<int64_t>(kMaxParts / 2, std::max<int64_t>(1, ceil_div(behind, fewest))));
+  // nothing is shared or split where a launch could not hold it: own_tiles alone fit one (checked before)
+  if ((p.prefix_groups() + requests * p.own_tiles * p.own_parts) * kv_heads >= kMaxGroups || p.line_rows >= kThreads / 64 * kMaxGroups)
+    return make_plan(requests, fresh, q_heads, kv_heads, max_len, 0, false, false);
   return p;
 }
 

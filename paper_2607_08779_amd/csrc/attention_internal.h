@@ -5,6 +5,8 @@
 
 namespace ssq {
 
+constexpr int64_t kMaxGroups = int64_t(1) << 24;     // workgroups of 256 threads: a grid holds fewer than 2^32 threads
+
 // Packed rows of heads: row t starts `stride` elements after row t - 1.
 template <typename T>
 struct Rows {

@@ -27,3 +27,17 @@ def test_page_tables_lengths_of_one_step_are_held_by_the_next():
         for bad in ([*now[:1], before[1], *now[2:]], [before[1].new_empty(n + 1), now[1], now[1], *now[3:]]):
             with pytest.raises(ssq.SSQError):
                 ssq.ssq_page_tables(before[1], ints([1] * n), dev_free, dev, page, n, taken=before[4], out=bad)
+
+
+def test_decode_of_as_many_requests_as_a_launch_holds():
+    """2^20 requests of 15 heads, a workgroup each: those of no token give zeros, of one token its value."""
+    n, heads, d, page = 1 << 20, 15, 64, 16
+    gen = torch.Generator(device="cuda").manual_seed(500)
+    k, v = (torch.randn((4, heads, page, d), generator=gen, device="cuda").bfloat16() for _ in "kv")
+    q = torch.randn((n, 1, heads, d), generator=gen, device="cuda", dtype=torch.bfloat16)
+    request = torch.arange(n, device="cuda", dtype=torch.int32)
+    lens, table = request % 2, (request % 4)[:, None].contiguous()
+    out = ssq.ssq_attention_decode(q, k, v, table, lens, page)
+    assert not out[::2].any()
+    for r in (1, 3):
+        assert (out[r::4, 0] == v[r, :, 0]).all()

@@ -557,6 +557,8 @@ def ssq_attention_decode(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.
         size = lib().ssq_attention_decode_workspace_size(n, fresh, hq, hk, dim, max_len, prefix)
         if size:
             workspace = torch.empty(size, dtype=torch.uint8, device=q.device)
+    elif not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
     stride = q.stride(1) if fresh > 1 else q.stride(0) if n > 1 else hq * dim
     shape = k_pages.shape
     st = fn(_ptr(q), stride, n, fresh, hq, hk, dim, dim ** -0.5 if scale is None else scale, _flat(k_pages, "k_pages", dtype, shape),

@@ -390,7 +390,7 @@ def _heads(t: torch.Tensor, what: str, dtype: torch.dtype, tokens: Optional[int]
     if tokens is not None and n != tokens:
         raise ValueError(f"{what} has {n} tokens, not {tokens}")
     rows, between, one = t.stride()
-    if one != 1 or between != dim:
+    if one != 1 or (between != dim and heads > 1):
         raise ValueError(f"the heads of a token of {what} must be contiguous")
     return rows if n > 1 else heads * dim
 
@@ -539,7 +539,7 @@ def ssq_attention_decode(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.
     where it is not given; ``scale`` defaults to 1 / sqrt(head_dim)."""
     dtype = q.dtype
     fn, name = _entry("ssq_attention_decode", dtype)
-    if q.dim() != 4 or q.stride(3) != 1 or q.stride(2) != q.shape[3] or (
+    if q.dim() != 4 or q.stride(3) != 1 or (q.stride(2) != q.shape[3] and q.shape[2] > 1) or (
             q.shape[0] > 1 and q.shape[1] > 1 and q.stride(0) != q.shape[1] * q.stride(1)):
         raise ValueError("q must be [requests, fresh, q_heads, head_dim], its tokens equally far apart and each contiguous")
     n, fresh, hq, dim = q.shape

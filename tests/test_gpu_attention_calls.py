@@ -41,3 +41,18 @@ def test_decode_of_as_many_requests_as_a_launch_holds():
     assert not out[::2].any()
     for r in (1, 3):
         assert (out[r::4, 0] == v[r, :, 0]).all()
+
+
+def test_one_head_of_a_tensor_of_heads_first():
+    """[heads, tokens, dim] transposed: with one head a token's row, whatever the stride between heads."""
+    gen = torch.Generator(device="cuda").manual_seed(510)
+    q, k, v = (torch.randn((1, 60, 64), generator=gen, device="cuda").bfloat16()[:, 3:53].transpose(0, 1) for _ in "qkv")
+    starts = ints([0, 30, 50])
+    A.check(ssq.ssq_attention_prompt(q, k, v, starts), *A.prompt_reference(q, k, v, [30, 20]), "one head")
+    pos, rope = torch.arange(50, device="cuda", dtype=torch.int32), torch.randn((50, 64), generator=gen, device="cuda")
+    for a, b in zip(ssq.ssq_qk_norm_rope(q, k, pos, rope), ssq.ssq_qk_norm_rope(q.clone().contiguous(), k.clone().contiguous(), pos, rope)):
+        assert torch.equal(a, b)
+    pools = [torch.randn((4, 1, 16, 64), generator=gen, device="cuda").bfloat16() for _ in "kv"]
+    table, lens = ints([[r % 4, 3] for r in range(50)]), [r % 33 for r in range(50)]
+    out = ssq.ssq_attention_decode(q[:, None], *pools, table, ints(lens), 32)
+    A.check(out, *A.decode_reference(q[:, None], *pools, table.cpu(), lens, 32, 0), "one head, decoding")

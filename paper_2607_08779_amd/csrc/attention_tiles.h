@@ -145,7 +145,8 @@ __device__ __forceinline__ Descriptor describe(const void* base, uint32_t bytes)
 __device__ __forceinline__ void load_lds(const Descriptor& d, uint8_t* to, uint32_t offset) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
                :
-               : "s"((uint32_t)(uintptr_t)(lds_void)to), "v"(offset), "s"(d));
+               : "s"((uint32_t)(uintptr_t)(lds_void)to), "v"(offset), "s"(d)
+               : "m0");
 }
 
 // Loads of 16 keys into LDS by one wavefront: `stride` bytes between rows, row0 the first row of

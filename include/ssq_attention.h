@@ -101,7 +101,8 @@ int ssq_page_tables(const int32_t* held, const int32_t* added, int64_t requests,
  *   positions       device, int32 [tokens]
  *   rope            device, binary32 [rope_rows, head_dim]: cosines, then sines; a
  *                   position outside [0, rope_rows) gives NaN
- *   q_out, k_out    device, bf16, written; may be q and k themselves with their strides;
+ *   q_out, k_out    device, bf16, written; may be q and k themselves with their strides
+ *                   (no other array that is written may overlap one that is read);
  *                   k_out may be NULL if a cache is given
  *   slots           device, int32 [tokens], or NULL (then so are the caches); a slot outside
  *                   [0, pages * page_size) is not stored
@@ -129,8 +130,9 @@ int ssq_qk_norm_rope_f32(const float* q, int64_t q_stride, const float* k, int64
  * for token i of a sequence and query head h of key/value head h / group,
  *   out_i = sum_{j <= i} w_j v_j,   w = softmax_j(scale q_i . k_j),   j in the same sequence.
  * Scores, maxima, sums and outputs are held in binary32; the weights are rounded to bf16
- * for the product with v (as the values are), relative to a running maximum, and divided by
- * the sum of the rounded ones.
+ * for the product with v (as the values are), relative to a running reference, and divided by
+ * the sum of the rounded ones.  Weights are up to 2^8 before that division, so that a result
+ * may be infinite where 2^8 sum_j |v_j| reaches 2^128.
  *
  *   starts    device, int32 [requests + 1], ascending from 0: sequence r holds the
  *             tokens starts[r] ... starts[r + 1] - 1 (none is valid); values are clamped to

@@ -1,8 +1,10 @@
 // Attention of a few new tokens of each request over the paged cache, with a prefix that all
 // requests share (see include/ssq_attention.h).
 //
-// The cache is read once, and its bytes are the floor.  Two kinds of workgroups share one
-// launch, and a second launch joins what they found, where there is more than one part:
+// The cache's bytes are the floor: keys are loaded once for each tile of rows, the prefix for 128
+// rows of all requests (32 in binary32), a request's own keys for 32 rows of it.  Two kinds of
+// workgroups share one launch, and a second launch joins what they found, where there is more than
+// one part:
 //
 // * wide: 128 query rows (all requests' new tokens and the group's heads) against a stretch
 //   of the shared prefix, 64 keys at a time through two stages of LDS that the four
@@ -11,7 +13,8 @@
 //   are no more than 32 in all, and in binary32) against a stretch of keys that the four
 //   wavefronts take 32 at a time, each through LDS of its own and without barriers: the next
 //   keys are loaded as soon as the scores of these are formed, the next values after the
-//   product.  Rows beside the used ones cost nothing that is scarce here.
+//   product.  In bf16 rows beside the used ones cost nothing that is scarce; in binary32, whose
+//   products run at a sixteenth of the rate, they do (one user's 16383 tokens 37 us, 26 of bytes).
 //
 // Bound by memory where the keys are the requests' own: one user's 16383 tokens (8 heads of 128)
 // take 18 us, of which 9.7 are the walk over the keys at 6.9 TB/s, the rest the start, the end and
@@ -61,6 +64,8 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // is written and read again.  So parts grow until the CUs have a workgroup each; beyond that, only
 // where whole tiles fill them badly (18 x 8 tiles behind 9589 keys, 79 requests of 7 tokens: 3 parts
 // 115 us, 2 parts 147, 4 parts 138; 2 x 8 tiles behind 8192 keys: 16 parts 41.8 us, 24 parts 46.3).
+// The fit is that of bf16 and tiles of 128 rows.  Binary32 takes the same number of parts, in tiles of 32
+// rows, one workgroup a CU in heads of 128, without a fit of its own (16 users behind 4096 tokens 42 us).
 int choose_prefix_parts(int64_t tiles, int64_t prefix, int64_t line_rows) {
   const int64_t most = std::min<int64_t>(kMaxParts / 2, ceil_div(prefix, 256));
   int best = 1;
@@ -410,8 +415,8 @@ hipError_t launch(const Decode<T>& a, void* workspace, size_t workspace_bytes, h
   const int64_t prefix_groups = p.prefix_groups(), own_groups = a.requests * p.own_tiles * p.own_parts;
   // Longest requests first where workgroups outnumber their places, two on each of 256 CUs, and the
   // longest walk 512 keys or more: 64 users of 1 to 1024 tokens behind 8192 (8 key/value heads)
-  // 53.8 -> 49.4 us, 32 of up to 2048 behind 4096 (64 heads) 46.1 -> 40.6.  Shorter walks do not gain
-  // what finding the order takes: 128 requests of up to 100 tokens 43.6 -> 47.0.
+  // 54.2 -> 49.4 us, 32 of up to 2048 behind 4096 (64 heads) 45.8 -> 41.0.  Shorter walks do not gain
+  // what finding the order takes: 128 requests of up to 100 tokens 14.5 -> 17.3, behind 4096 32.0 -> 34.4.
   const int64_t behind = a.max_len - std::min(a.max_len, p.share != kShareNone ? a.prefix : 0);
   const bool sorted = a.requests > 1 && (prefix_groups + own_groups) * a.kv_heads > 512 && behind / p.own_parts >= 512;
   decode_kernel<T, D><<<dim3((unsigned)((prefix_groups + own_groups) * a.kv_heads)), kThreads, 0, stream>>>(a, p, parts, (int)prefix_groups, sorted);

@@ -188,21 +188,23 @@ void launch_kernel(const Prompt<float>& a, int group, hipStream_t stream) {
   launch_small<float, D>(a, group, stream);
 }
 
-// In bf16 that form loads each key four times as often.  It pays where its workgroups are all
-// resident at once and sequences are long for their number, as with the few key/value heads of
-// a small model or of a shard: there a row tile's time is one walk over its keys, which the
-// wavefronts then share (us, 128 rows -> 32 rows a workgroup, one sequence):
+// In bf16 that form loads each key four times as often.  It pays where its workgroups are few and
+// sequences are long for their number, as with the few key/value heads of a small model or of a
+// shard: there a row tile's time is one walk over its keys, which the wavefronts then share.  The bound
+// of 768 workgroups is between what was measured to gain and to lose, for both head sizes (of 128
+// two are resident on a CU, of 64 four).  us, 128 rows -> 32 rows a workgroup, one sequence:
 //   2 kv heads of 128, group 4: 400 tokens 10.7 -> 9.7, 1000 20.1 -> 13.5, 3000 49.8 -> 36.8
+//   4 kv heads of 128, group 4: 1400 tokens (704 workgroups) 26.2 -> 24.5; 2000 (1004) 35.4 -> 36.7: not taken
 //   8 kv heads of 128, group 4: 400 tokens 11.1 -> 11.5, 1000 21.4 -> 26.5: not taken
 //   8 kv heads of 64, group 1: 100 tokens 5.5 -> 4.9, 1000 14.9 -> 9.6
-//   8 kv heads of 64, group 4: 700 tokens 11.6 -> 10.1, 1000 15.3 -> 17.4: not taken
+//   8 kv heads of 64, group 4: 700 tokens (704) 11.6 -> 10.1; 1000 (1008) 15.3 -> 17.4: not taken
 // and short sequences (16 of 47 tokens in the mean, 2 kv heads of 128: 6.2 -> 7.2) lose.
 template <int D>
 bool prefers_small(const Prompt<uint16_t>& a, int group) {
   if (a.requests == 0) return false;
   const int64_t groups = small_groups(a, group), mean = a.tokens / a.requests;
-  constexpr int64_t kResident = 3 * 256;
-  return D == 64 ? mean >= 96 && groups <= std::min(kResident, mean * 8 / 7) : mean >= 320 && groups <= std::min(kResident, mean);
+  constexpr int64_t kMost = 768;
+  return D == 64 ? mean >= 96 && groups <= std::min(kMost, mean * 8 / 7) : mean >= 320 && groups <= std::min(kMost, mean);
 }
 template <int D>
 void launch_kernel(const Prompt<uint16_t>& a, int group, hipStream_t stream) {

@@ -15,7 +15,11 @@
 // maximum of that row exceeds it by more than kSlack: weights stay at or below 2^kSlack, far from any
 // overflow.  In bf16 the weights are rounded to 8 significant bits for the product, because the
 // matrix cores take both operands in one type; each is off by up to 2^-9 of itself, whatever m is,
-// though by how much depends on m's fraction.
+// though by how much depends on m's fraction.  A second product with what the rounding leaves was
+// measured and not taken: results come from 2.0e-3 to 1.65e-3 of those in 64 bits (relative norm; the
+// output's own rounding is 1.63e-3), and eight ragged prompts go from 252 to 315 us, a prompt of 16384
+// tokens from 1.96 to 2.68 ms, one user's 16383 cached tokens from 17.8 to 18.9 us, 64 users behind
+// 8192 from 49.2 to 51.2, eight requests of 100 to 300 from 7.8 to 8.5.
 //
 // The sum starts at -0 and leaves it with the first tile of which the row sees a key.  So a sum of -0
 // is that of a row that saw none, which gives zeros, and +0 that of one whose scores were all -inf,
@@ -415,9 +419,9 @@ struct Rows32 {
     }
   }
 
-  // Weights of 32 KT keys, one of which the row sees or none, from their scores, and the running sum.  The sum is that of the weights as
-  // the product takes them, so that their rounding is one of weights that still add up to one
-  // (in bf16: a row of one or a few keys comes out as exact as its values are).
+  // Weights of 32 KT keys from their scores, and the running sum; `seen`: the row sees one of them.
+  // The sum is that of the weights as the product takes them, so that their rounding is one of weights
+  // that still add up to one (in bf16: a row of one or a few keys comes out as exact as its values are).
   template <int KT>
   __device__ __forceinline__ void weights(const f32x16 (&s)[KT], float scale, bool seen, typename P::template Weights<KT>& p) {
     float sum[2] = {0.0f, 0.0f};

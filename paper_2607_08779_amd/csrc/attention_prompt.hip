@@ -8,8 +8,8 @@
 // while this one is used.  Two workgroups share a CU, so that one's softmax runs beside the
 // other's products.
 //
-// Bound by arithmetic.  One prompt of 16384 tokens (32/8 heads of 128) takes 1.95 ms, 1120 TFLOP/s of
-// the causal half, where a matrix product of 8192^3 random values reaches 1200: at both the
+// Bound by arithmetic.  One prompt of 16384 tokens (32/8 heads of 128) takes 1.95 to 2.0 ms by card,
+// 1100 to 1130 TFLOP/s of the causal half, where a matrix product of 8192^3 random values reaches 1200: at both the
 // card's power sets the clock (1.5 to 1.6 GHz here; the matrix cores are busy in 60 % of its cycles).
 // Eight prompts of 300 to 2048 tokens (64/8 heads) take 250 us, 856 TFLOP/s: a workgroup's tiles
 // take 1.57 us each, and looking up its place, its first loads, its edge and its end 6.8.

@@ -32,6 +32,9 @@
  *   - Keys that a query does not see have no influence on its result, whatever their
  *     bits (infinities and NaN included): it is the same to the last bit.  A query that
  *     sees no key gives zeros; one whose scores are all -infinity gives NaN.
+ *   - Up to 2^20 requests are taken, but the calls are made for some thousands: each
+ *     workgroup of ssq_attention_prompt and ssq_page_tables walks the requests' starts or
+ *     lengths (64 and 1024 at a time) up to its own, so their time grows with the square.
  */
 #ifndef SSQ_ATTENTION_H
 #define SSQ_ATTENTION_H

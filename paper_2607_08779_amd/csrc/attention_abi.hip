@@ -2,43 +2,11 @@
 // include/ssq_attention.h).  Every check runs on the host before any HIP call.
 #include "ssq_attention.h"
 
-#include <cmath>
-
-#include "attention_internal.h"
+#include "attention_checks.h"
 
 namespace {
 
-constexpr int64_t kMaxRequests = int64_t(1) << 20;
-constexpr int64_t kMaxRows = int64_t(1) << 31;       // kernels index rows in int
 constexpr int64_t kMaxRopeBytes = int64_t(127) << 30; // of all heads: 32 bytes a thread, of which a grid holds fewer than 2^32
-constexpr int64_t kMaxStride = int64_t(1) << 24;     // elements between rows (32-bit tile offsets)
-constexpr int64_t kMaxLen = int64_t(1) << 30;
-constexpr int kMaxHeadCount = 1 << 16;
-
-bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
-int status_of(hipError_t e) { return e == hipSuccess ? SSQ_OK : SSQ_EHIP; }
-bool valid_dim(int d) { return d == 64 || d == 128; }
-bool valid_page(int p) { return p >= 16 && p <= 1024 && (p & (p - 1)) == 0; }
-bool valid_heads(int q_heads, int kv_heads) {
-  return q_heads > 0 && kv_heads > 0 && q_heads <= kMaxHeadCount && q_heads % kv_heads == 0;
-}
-int shift_of(int page_size) { return __builtin_ctz((unsigned)page_size); }
-
-// An array of 4-byte elements, which may be empty.
-struct Span {
-  const void* p;
-  int64_t count;
-};
-bool overlap(const Span& a, const Span& b) {
-  const auto x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
-  return a.count > 0 && b.count > 0 && x < y + 4 * (uintptr_t)b.count && y < x + 4 * (uintptr_t)a.count;
-}
-
-// Rows of `heads` heads: a stride that holds them, in whole 16-byte pieces.
-template <typename T>
-bool valid_stride(int64_t stride, int heads, int head_dim) {
-  return stride >= (int64_t)heads * head_dim && stride <= kMaxStride && stride % (int64_t)(16 / sizeof(T)) == 0;
-}
 
 int check_page_tables(const int32_t* held, const int32_t* added, int64_t requests, const int32_t* free_pages,
                       int64_t free_count, const int32_t* taken, int page_size, const int32_t* table, int64_t table_stride,
@@ -114,14 +82,6 @@ int prompt(const T* q, int64_t q_stride, const T* k, int64_t k_stride, const T* 
   if (!aligned(starts, 4)) return SSQ_EALIGN;
   const ssq::Prompt<T> a = {{q, q_stride}, {k, k_stride}, {v, v_stride}, {out, out_stride}, starts, requests, tokens, q_heads, kv_heads, scale};
   return status_of(ssq::launch_attention_prompt(a, head_dim, stream));
-}
-
-bool valid_decode_sizes(int64_t requests, int fresh, int q_heads, int kv_heads, int head_dim, int64_t max_len, int64_t prefix) {
-  if (requests < 0 || requests > kMaxRequests || fresh < 1 || !valid_heads(q_heads, kv_heads) || !valid_dim(head_dim) ||
-      max_len < 0 || max_len > kMaxLen || prefix < 0)
-    return false;
-  return fresh <= kMaxLen && requests * fresh < kMaxRows &&
-         requests * fresh * q_heads + 32 * requests * kv_heads < 32 * ssq::kMaxGroups;      // own rows, 32 a workgroup
 }
 
 template <typename T>

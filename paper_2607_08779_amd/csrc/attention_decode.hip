@@ -21,13 +21,9 @@
 // the launch that joins.  64 users behind a shared prefix of 8192 tokens, 1 to 1024 of their own,
 // take 42 us where the cache lies partly in the Infinity Cache and 49 where it does not (175 MB,
 // 3.6 TB/s): workgroups of 2 to 20 us of work on 512 places end unevenly.
-//
-// Parts leave O unnormalised in binary32 with its reference and sum, and are joined as
-//   out = sum_s 2^(m_s - M) O_s / sum_s 2^(m_s - M) l_s,   M = max_s m_s.
 #include <algorithm>
-#include <type_traits>
 
-#include "attention_tiles.h"
+#include "attention_join.h"
 
 namespace ssq {
 namespace attention {
@@ -35,8 +31,6 @@ namespace {
 
 constexpr int kWaves = 4, kThreads = 64 * kWaves, kWideRows = 32 * kWaves, kWideKeys = 64, kNarrowRows = 32;
 constexpr int kNarrowKeys = 32 * kWaves;              // keys that a narrow workgroup takes at a time
-constexpr int kMaxParts = 64;
-constexpr int64_t kWaveJoinRows = 1536;               // rows of out from which a wavefront joins a row
 
 enum Share : int { kShareNone = 0, kShareWide, kShareNarrow };
 
@@ -50,13 +44,6 @@ struct Plan {
   int parts() const { return own_parts + (share != kShareNone ? prefix_parts : 0); }
   int64_t prefix_groups() const { return share != kShareNone ? (int64_t)prefix_tiles * prefix_parts : 0; }
 };
-
-struct Parts {           // of every row: [part][row] and [part][row][D]
-  float2* ml;            // null: one part, straight to out
-  float* o;
-};
-
-int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // Parts of the prefix, for `tiles` workgroups a part: the quickest by a fit of its time (us).  A
 // tile of 64 keys takes a workgroup 1.1 where it has a CU to itself and 1.57 where it shares one, of
@@ -113,14 +100,6 @@ Plan make_plan(int64_t requests, int fresh, int q_heads, int kv_heads, int64_t m
   return p;
 }
 
-// Rows of this wavefront: lane's column, where it goes and the last key it sees.
-struct Row {
-  bool present;
-  int64_t line;          // row of q and out
-  int column;            // head
-  int last;
-};
-
 // The pages of one table row, and the descriptors of 16 keys in them.
 // The entry is read through the constant address space: a scalar load, which does not wait
 // behind the loads of keys and values in flight as a vector load's result would.
@@ -137,41 +116,6 @@ struct Pages {
 template <typename T, int D>
 __device__ __forceinline__ int64_t group_offset(const Decode<T>& a, int head, int64_t page, int j) {
   return (((page * a.kv_heads + head) << a.cache.page_shift) + (j & ((1 << a.cache.page_shift) - 1))) * D;
-}
-
-template <typename T>
-__device__ __forceinline__ int request_len(const Decode<T>& a, int request) {
-  const int64_t room = min(a.max_len, a.table_stride << a.cache.page_shift);
-  return (int)min((int64_t)max(a.lens[request], 0), room);
-}
-
-// The request that takes place `i` where those of each 64 stand longest first, so that what starts
-// last is short.
-template <typename T>
-__device__ __forceinline__ int longest_first(const Decode<T>& a, int i) {
-  const int lane = threadIdx.x & 63, base = i & ~63, r = base + lane;
-  const bool there = r < a.requests;
-  const uint32_t key = (there ? (uint32_t)(min(max(a.lens[there ? r : base], 0), (1 << 25) - 1) + 1) << 6 : 0u) | (uint32_t)(63 - lane);
-  int before = 0;
-#pragma unroll 16
-  for (int j = 0; j < 64; ++j) before += (uint32_t)__builtin_amdgcn_readlane((int)key, j) > key ? 1 : 0;
-  return base + __builtin_ctzll(__builtin_amdgcn_ballot_w64(before == (i & 63)));
-}
-
-// Four consecutive outputs of a row, of one part or of all.
-template <typename T, int D>
-__device__ __forceinline__ void put(const Decode<T>& a, const Plan& p, const Parts& parts, int part, const Row& row,
-                                    int at, f32x4 o, float m, float l) {
-  if (parts.ml == nullptr) {
-    const float by = inverse_of(l);
-    T* to = a.out.p + row.line * a.out.stride + row.column * D + at;
-    if constexpr (sizeof(T) == 2) *reinterpret_cast<u32x2*>(to) = u32x2{pack_bf16x2(o[0] * by, o[1] * by), pack_bf16x2(o[2] * by, o[3] * by)};
-    else *reinterpret_cast<f32x4*>(to) = f32x4{o[0] * by, o[1] * by, o[2] * by, o[3] * by};
-  } else {
-    const int64_t r = part * p.line_rows + row.line * a.q_heads + row.column;
-    *reinterpret_cast<f32x4*>(parts.o + r * D + at) = o;
-    if (at == 0) parts.ml[r] = float2{m, l};
-  }
 }
 
 template <typename T, int D>
@@ -233,7 +177,7 @@ __device__ void wide(const Decode<T>& a, const Plan& p, const Parts& parts, int 
   for (int t = 0; t < S::kOut; ++t)
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      put<T, D>(a, p, parts, part, row, 32 * t + 8 * i + 4 * (lane / 32), f32x4{r.o[t][4 * i], r.o[t][4 * i + 1], r.o[t][4 * i + 2], r.o[t][4 * i + 3]}, r.m, l);
+      put<T, D>(a, p.line_rows, parts, part, row, 32 * t + 8 * i + 4 * (lane / 32), f32x4{r.o[t][4 * i], r.o[t][4 * i + 1], r.o[t][4 * i + 2], r.o[t][4 * i + 3]}, r.m, l);
 }
 
 // Keys [begin, end) of a table row.
@@ -292,7 +236,7 @@ __device__ void narrow(const Decode<T>& a, const Plan& p, const Parts& parts, in
   walk(std::false_type{});
   if (__builtin_amdgcn_ballot_w64(row.present && r.spoiled()) != 0) walk(std::true_type{});
   join_waves<kWaves>(r, lds, ml, min(rows - index0, kNarrowRows), wave, lane,
-                     [&](int of, int at, f32x4 o, float m, float l) { put<T, D>(a, p, parts, part, find_row(of), at, o, m, l); });
+                     [&](int of, int at, f32x4 o, float m, float l) { put<T, D>(a, p.line_rows, parts, part, find_row(of), at, o, m, l); });
 }
 
 template <typename T, int D>
@@ -341,62 +285,8 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void decode_kerne
   narrow<T, D>(a, p, parts, head, request, index0, range, part, lds, ml);
 }
 
-// One row of out from its parts, by R lanes, a wavefront or a workgroup of them: D / 4 lanes hold the
-// row, and the groups of so many lanes take the parts in turn, so that their loads are under way
-// together.
-template <typename T, int D, int R>
-__global__ __launch_bounds__(kThreads) void join_kernel(const Decode<T> a, int64_t line_rows, int count, const Parts parts) {
-  constexpr int kLanes = D / 4, kGroups = R / kLanes;
-  const int lane = threadIdx.x & 63, at = (int)threadIdx.x % kLanes, group = (int)threadIdx.x % R / kLanes;
-  const int64_t row = blockIdx.x * (int64_t)(kThreads / R) + threadIdx.x / R;
-  if (row >= line_rows) return;               // whole wavefronts; none where a workgroup holds a row
-  const float* from = parts.o + row * D + 4 * at;
-  constexpr int kAhead = R == 64 ? 8 : 4;
-  f32x4 o[kAhead];
-#pragma unroll
-  for (int i = 0; i < kAhead; ++i) {
-    const int s = group + i * kGroups;
-    o[i] = s < count ? *reinterpret_cast<const f32x4*>(from + s * line_rows * D) : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  }
-  // every wavefront forms the parts' weights, for itself
-  const float2 x = lane < count ? parts.ml[lane * line_rows + row] : float2{-FLT_MAX, __uint_as_float(kSawNone)};
-  const float m = wave_max(x.y != 0.0f ? x.x : -FLT_MAX);
-  const float by = x.y != 0.0f ? __builtin_amdgcn_exp2f(x.x - m) : 0.0f;
-  float l = wave_sum(by * x.y);
-  if (l == 0.0f && __builtin_amdgcn_ballot_w64(__float_as_uint(x.y) != kSawNone) == 0) l = __uint_as_float(kSawNone);
-  f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-  for (int i = 0; i < kMaxParts / kGroups; ++i) {
-    const int s = group + i * kGroups;
-    if (i * kGroups >= count) break;
-    const float w = __shfl(by, s, 64);
-    const f32x4 y = i < kAhead ? o[i] : s < count ? *reinterpret_cast<const f32x4*>(from + s * line_rows * D) : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-    for (int e = 0; e < 4; ++e) sum[e] = __builtin_fmaf(w, y[e], sum[e]);
-  }
-  if constexpr (R == 64) {
-#pragma unroll
-    for (int d = kLanes; d < 64; d <<= 1)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) sum[e] += __shfl_xor(sum[e], d, 64);
-  } else {
-    __shared__ f32x4 sums[kGroups][kLanes];
-    sums[group][at] = sum;
-    __syncthreads();
-    if (group != 0) return;
-#pragma unroll
-    for (int g = 1; g < kGroups; ++g)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) sum[e] += sums[g][at][e];
-  }
-  if (group != 0) return;
-  const int64_t line = row / a.q_heads;
-  const Row to = {true, line, (int)(row - line * a.q_heads), 0};
-  put<T, D>(a, Plan{}, Parts{nullptr, nullptr}, 0, to, 4 * at, sum, 0.0f, l);
-}
-
 size_t part_bytes(const Plan& p, int head_dim) {
-  return p.parts() > 1 ? (size_t)p.parts() * (size_t)p.line_rows * (8 + 4 * (size_t)head_dim) : 0;
+  return parts_bytes(p.parts(), p.line_rows, head_dim);
 }
 
 template <typename T, int D>
@@ -407,11 +297,7 @@ hipError_t launch(const Decode<T>& a, void* workspace, size_t workspace_bytes, h
     p = make_plan(a.requests, a.fresh, a.q_heads, a.kv_heads, a.max_len, a.prefix, false, false);
     need = 0;
   }
-  Parts parts = {nullptr, nullptr};
-  if (need > 0) {
-    parts.o = static_cast<float*>(workspace);
-    parts.ml = reinterpret_cast<float2*>(parts.o + (size_t)p.parts() * p.line_rows * D);
-  }
+  const Parts parts = need > 0 ? place_parts<D>(workspace, p.parts(), p.line_rows) : Parts{nullptr, nullptr};
   const int64_t prefix_groups = p.prefix_groups(), own_groups = a.requests * p.own_tiles * p.own_parts;
   // Longest requests first where workgroups outnumber their places, two on each of 256 CUs, and the
   // longest walk 512 keys or more: 64 users of 1 to 1024 tokens behind 8192 (8 key/value heads)
@@ -420,14 +306,7 @@ hipError_t launch(const Decode<T>& a, void* workspace, size_t workspace_bytes, h
   const int64_t behind = a.max_len - std::min(a.max_len, p.share != kShareNone ? a.prefix : 0);
   const bool sorted = a.requests > 1 && (prefix_groups + own_groups) * a.kv_heads > 512 && behind / p.own_parts >= 512;
   decode_kernel<T, D><<<dim3((unsigned)((prefix_groups + own_groups) * a.kv_heads)), kThreads, 0, stream>>>(a, p, parts, (int)prefix_groups, sorted);
-  if (need > 0) {
-    // A wavefront a row where the rows fill the chip (2560 rows of 7 parts: a step of 20.3 us against
-    // 21.2 with a workgroup a row), a workgroup a row where they do not (32 rows of 32 parts: 18.9
-    // against 21.9; equal at about 1000 rows).
-    constexpr int kPerGroup = kThreads / 64;
-    if (p.line_rows >= kWaveJoinRows) join_kernel<T, D, 64><<<dim3((unsigned)((p.line_rows + kPerGroup - 1) / kPerGroup)), kThreads, 0, stream>>>(a, p.line_rows, p.parts(), parts);
-    else join_kernel<T, D, kThreads><<<dim3((unsigned)p.line_rows), kThreads, 0, stream>>>(a, p.line_rows, p.parts(), parts);
-  }
+  if (need > 0) launch_join<T, D>(a, p.line_rows, p.parts(), parts, stream);
   return hipGetLastError();
 }
 

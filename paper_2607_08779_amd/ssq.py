@@ -526,6 +526,14 @@ def ssq_attention_decode_workspace_size(requests: int, fresh: int, q_heads: int,
     return int(lib().ssq_attention_decode_workspace_size(requests, fresh, q_heads, kv_heads, head_dim, max_len, prefix))
 
 
+def _fresh_rows(q: torch.Tensor) -> int:
+    """Elements between the tokens of q [requests, fresh, q_heads, head_dim]."""
+    if q.dim() != 4 or q.stride(3) != 1 or (q.stride(2) != q.shape[3] and q.shape[2] > 1) or (
+            q.shape[0] > 1 and q.shape[1] > 1 and q.stride(0) != q.shape[1] * q.stride(1)):
+        raise ValueError("q must be [requests, fresh, q_heads, head_dim], its tokens equally far apart and each contiguous")
+    return q.stride(1) if q.shape[1] > 1 else q.stride(0) if q.shape[0] > 1 else q.shape[2] * q.shape[3]
+
+
 def ssq_attention_decode(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, table: torch.Tensor,
                          lens: torch.Tensor, max_len: int, prefix: int = 0, scale: Optional[float] = None,
                          out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
@@ -539,9 +547,7 @@ def ssq_attention_decode(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.
     where it is not given; ``scale`` defaults to 1 / sqrt(head_dim)."""
     dtype = q.dtype
     fn, name = _entry("ssq_attention_decode", dtype)
-    if q.dim() != 4 or q.stride(3) != 1 or (q.stride(2) != q.shape[3] and q.shape[2] > 1) or (
-            q.shape[0] > 1 and q.shape[1] > 1 and q.stride(0) != q.shape[1] * q.stride(1)):
-        raise ValueError("q must be [requests, fresh, q_heads, head_dim], its tokens equally far apart and each contiguous")
+    stride = _fresh_rows(q)
     n, fresh, hq, dim = q.shape
     if k_pages.dim() != 4 or k_pages.shape[3] != dim:
         raise ValueError("the caches must be [pages, kv_heads, page_size, head_dim]")
@@ -559,7 +565,6 @@ def ssq_attention_decode(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.
             workspace = torch.empty(size, dtype=torch.uint8, device=q.device)
     elif not workspace.is_contiguous():
         raise ValueError("workspace must be contiguous")
-    stride = q.stride(1) if fresh > 1 else q.stride(0) if n > 1 else hq * dim
     shape = k_pages.shape
     st = fn(_ptr(q), stride, n, fresh, hq, hk, dim, dim ** -0.5 if scale is None else scale, _flat(k_pages, "k_pages", dtype, shape),
             _flat(v_pages, "v_pages", dtype, shape), pages, page_size, _flat(table, "table", torch.int32, (n, width)), width,
@@ -568,3 +573,229 @@ def ssq_attention_decode(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.
     if st:
         _check(name, st)
     return out
+
+
+# --- the paged cache in 4 bits, and pages of any cache (include/ssq_cache.h) -------------------
+
+for _name, _args in (("ssq_kv4_store", [_P, _L, _P, _L, _L, _I, _I, _P, _P, _L, _I, _P, _L, _P, _L, _P]),
+                     ("ssq_attention_decode_kv4", [_P, _L, _L, _I, _I, _I, _I, _F, _P, _L, _I, _P, _L, _P, _L, _L, _P, _L, _P,
+                                                   ctypes.c_size_t, _P])):
+    _EXPORTS[_name] = _EXPORTS[_name + "_f32"] = (_I, _args)
+_EXPORTS["ssq_attention_decode_kv4_workspace_size"] = _EXPORTS["ssq_attention_decode_workspace_size"]
+_EXPORTS["ssq_page_fork"] = (_I, [_P, _L, _P, _P, _L, _L, _P, _L, _P, _I, _P, _L, _P, _P, _P, _P, _P])
+_EXPORTS["ssq_page_collect"] = (_I, [_P, _L, _P, _L, _I, _L, _P, _P, _P, _P, ctypes.c_size_t, _P])
+_EXPORTS["ssq_page_compact"] = (_I, [_P, _L, _P, _L, _I, _L, _P, _P, _P, _P, _P, _P, _P, _P, ctypes.c_size_t, _P])
+_EXPORTS["ssq_page_collect_workspace_size"] = (ctypes.c_size_t, [_L, _I])
+_EXPORTS["ssq_page_copy"] = (_I, [_P, _I, _L, _L, _P, _P, _L, _P])
+
+
+def _launch(fn, name: str, device: torch.device, tensors, *args) -> None:
+    """fn(*args, stream) on the current stream of `device`, where all of `tensors` (or None) have to be."""
+    for t in tensors:
+        if t is not None and t.device != device:
+            raise ValueError(f"all tensors must be on one device (got {device} and {t.device})")
+    if device.index == torch.cuda.current_device():
+        st = fn(*args, _stream(device))
+    else:
+        with torch.cuda.device(device):
+            st = fn(*args, _stream(device))
+    if st:
+        _check(name, st)
+
+
+def ssq_kv4_cache(pages: int, kv_heads: int, page_size: int, head_dim: int, device="cuda") -> torch.Tensor:
+    """An empty cache in 4 bits, of both keys and values: uint8 [pages, kv_heads, 2,
+    page_size * 9 * head_dim // 16] (the layout is in include/ssq_cache.h)."""
+    return torch.zeros((pages, kv_heads, 2, page_size * 9 * head_dim // 16), dtype=torch.uint8, device=device)
+
+
+def _kv4(cache: torch.Tensor, heads: int, dim: int) -> Tuple[int, int, int]:
+    """Pointer, pages and page size of a 4-bit cache."""
+    if cache.dim() != 4 or cache.shape[1] != heads or cache.shape[2] != 2 or cache.shape[3] * 16 % (9 * dim or 1):
+        raise ValueError("the cache must be [pages, kv_heads, 2, page_size * 9 * head_dim // 16] of these heads")
+    return _flat(cache, "cache", torch.uint8, cache.shape), cache.shape[0], cache.shape[3] * 16 // (9 * dim or 1)
+
+
+def ssq_kv4_store(k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, cache: torch.Tensor, held=None):
+    """Keys and values [tokens, kv_heads, head_dim] (bf16 or fp32; tokens may be strided) onto the signed
+    absmax grid in 4 bits and into their ``slots`` (int32 [tokens]) of ``cache`` (``ssq_kv4_cache``), on the
+    current stream.  With ``held=True`` the rows as the cache holds them are returned, (k, v), for a
+    prompt's own attention; ``held`` = (k, v) writes them to those tensors, which may be k and v."""
+    dtype = k.dtype
+    fn, name = _entry("ssq_kv4_store", dtype)
+    ks, vs = _heads(k, "k", dtype), _heads(v, "v", dtype, k.shape[0])
+    tokens, hk, dim = k.shape
+    if v.shape != k.shape:
+        raise ValueError("v must be like k")
+    cp, pages, page_size = _kv4(cache, hk, dim)
+    khs = vhs = 0
+    khp = vhp = None
+    if held is True:
+        held = torch.empty_like(k, memory_format=_PACKED), torch.empty_like(v, memory_format=_PACKED)
+    if held:
+        if held[0].shape != k.shape or held[1].shape != v.shape:
+            raise ValueError("held must be tensors like k and v")
+        khs, vhs = _heads(held[0], "held k", dtype), _heads(held[1], "held v", dtype)
+        khp, vhp = _ptr(held[0]), _ptr(held[1])
+    _launch(fn, name, k.device, (v, slots, cache, *(held or ())), _ptr(k), ks, _ptr(v), vs, tokens, hk, dim,
+            _flat(slots, "slots", torch.int32, (tokens,)), cp, pages, page_size, khp, khs, vhp, vhs)
+    return held or None
+
+
+def ssq_attention_decode_kv4_workspace_size(requests: int, fresh: int, q_heads: int, kv_heads: int, head_dim: int,
+                                            max_len: int, prefix: int = 0) -> int:
+    """Bytes of scratch that let ssq_attention_decode_kv4 split long caches and share a prefix."""
+    return int(lib().ssq_attention_decode_kv4_workspace_size(requests, fresh, q_heads, kv_heads, head_dim, max_len, prefix))
+
+
+def ssq_attention_decode_kv4(q: torch.Tensor, cache: torch.Tensor, table: torch.Tensor, lens: torch.Tensor, max_len: int,
+                             prefix: int = 0, scale: Optional[float] = None, out: Optional[torch.Tensor] = None,
+                             workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """``ssq_attention_decode`` over a cache in 4 bits (``ssq_kv4_cache``): the same arguments, with one
+    ``cache`` in place of the two.  ``workspace`` (uint8, any contents,
+    ``ssq_attention_decode_kv4_workspace_size`` bytes) is allocated where it is not given."""
+    dtype = q.dtype
+    fn, name = _entry("ssq_attention_decode_kv4", dtype)
+    stride = _fresh_rows(q)
+    n, fresh, hq, dim = q.shape
+    if cache.dim() != 4 or table.dim() != 2:
+        raise ValueError("the cache must be [pages, kv_heads, 2, bytes] and table [requests, pages]")
+    hk, width = cache.shape[1], table.shape[1]
+    cp, pages, page_size = _kv4(cache, hk, dim)
+    if out is None:
+        out = torch.empty_like(q, memory_format=_PACKED)
+    elif out.shape != q.shape or out.dtype != dtype or not out.is_contiguous():
+        raise ValueError("out must be a contiguous tensor like q")
+    if workspace is None:
+        size = lib().ssq_attention_decode_kv4_workspace_size(n, fresh, hq, hk, dim, max_len, prefix)
+        if size:
+            workspace = torch.empty(size, dtype=torch.uint8, device=q.device)
+    elif not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
+    _launch(fn, name, q.device, (cache, table, lens, out, workspace), _ptr(q), stride, n, fresh, hq, hk, dim,
+            dim ** -0.5 if scale is None else scale, cp, pages, page_size, _flat(table, "table", torch.int32, (n, width)), width,
+            _flat(lens, "lens", torch.int32, (n,)), max_len, prefix, _ptr(out), hq * dim, _ptr(workspace),
+            0 if workspace is None else workspace.numel() * workspace.element_size())
+    return out
+
+
+def ssq_page_fork(parents: torch.Tensor, lens: torch.Tensor, table: torch.Tensor, free_pages: torch.Tensor, page_size: int,
+                  taken: Optional[torch.Tensor] = None, width: Optional[int] = None, out=None):
+    """Tables of requests that continue others, on the current stream: request i has the pages of row
+    ``parents[i]`` (int32; outside the rows: none) of ``table`` (int32 [rows, pages], ``lens`` [rows]
+    tokens), but a new page from ``free_pages`` (entry ``taken`` on) in place of a last page that is not full and
+    that an earlier request continues.  Returns (table [requests, width], lens, src, dst [requests], taken after [1]),
+    int32; ``width`` defaults to that of ``table``.  The pages src -> dst (-1: none) are to be copied in
+    every layer (``ssq_page_copy``).  ``out`` = these five reuses buffers, which must not be those of another argument."""
+    if parents.dim() != 1 or table.dim() != 2:
+        raise ValueError("parents must be [requests] and table [rows, pages]")
+    i32, dev, n = torch.int32, parents.device, parents.shape[0]
+    rows, stride = table.shape
+    if out is None:
+        width = stride if width is None else width
+        if width < 0:
+            raise ValueError("width must not be negative")
+        # one allocation, cut up
+        buf = torch.empty(n * width + 3 * n + 1, dtype=i32, device=dev)
+        table_out, lens_out, src, dst, after = torch.split_with_sizes(buf, (n * width, n, n, n, 1))
+        table_out = table_out.view(n, width)
+        at = _ptr(buf)
+        to = at, at + 4 * n * width, at + 4 * n * (width + 1), at + 4 * n * (width + 2), at + 4 * n * (width + 3)
+    else:
+        table_out, lens_out, src, dst, after = out
+        if table_out.dim() != 2 or (width is not None and table_out.shape[1] != width):
+            raise ValueError("out's table must be [requests, width]")
+        width = table_out.shape[1]
+        to = (_flat(table_out, "table out", i32, (n, width)), _flat(lens_out, "lens out", i32, (n,)), _flat(src, "src", i32, (n,)),
+              _flat(dst, "dst", i32, (n,)), _flat(after, "taken after", i32, (1,)))
+    fn, name = _entry("ssq_page_fork", torch.bfloat16)
+    _launch(fn, name, dev, (lens, table, free_pages, taken, table_out, lens_out, src, dst, after), _flat(parents, "parents", i32, (n,)), n,
+            _flat(lens, "lens", i32, (rows,)), _flat(table, "table", i32, (rows, stride)), rows, stride,
+            _flat(free_pages, "free_pages", i32, free_pages.shape[:1]), free_pages.numel(),
+            None if taken is None else _flat(taken, "taken", i32, (1,)), page_size, to[0], width, *to[1:])
+    return table_out, lens_out, src, dst, after
+
+
+def _pool_arguments(lens, table, pages, pinned, compact, workspace):
+    if lens.dim() != 1 or table.dim() != 2:
+        raise ValueError("lens must be [requests] and table [requests, pages]")
+    if pages < 0:
+        raise ValueError("pages must not be negative")
+    n, width = table.shape
+    if workspace is None:
+        workspace = torch.empty(lib().ssq_page_collect_workspace_size(pages, compact), dtype=torch.uint8, device=lens.device)
+    elif not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
+    return (_flat(lens, "lens", torch.int32, (n,)), n, _flat(table, "table", torch.int32, (n, width)), width,
+            None if pinned is None else _flat(pinned, "pinned", torch.uint8, (pages,)), workspace)
+
+
+def ssq_page_collect(lens: torch.Tensor, table: torch.Tensor, page_size: int, pages: int, pinned: Optional[torch.Tensor] = None,
+                     out=None, workspace: Optional[torch.Tensor] = None):
+    """The pages of a pool of ``pages`` that no request holds, on the current stream: request r holds the
+    first ceil(lens[r] / page_size) entries of ``table[r]`` (int32 [requests, pages]); ``pinned`` (uint8 [pages])
+    is not 0 for pages that are held in any case.  Returns (free_pages [pages], ascending, then -1; count [1]), int32.
+    ``out`` reuses buffers; ``workspace`` (uint8, any contents, ``ssq_page_collect_workspace_size`` bytes)
+    is allocated where it is not given."""
+    lp, n, tp, width, pp, workspace = _pool_arguments(lens, table, pages, pinned, 0, workspace)
+    i32 = torch.int32
+    if out is None:
+        buf = torch.empty(pages + 1, dtype=i32, device=lens.device)
+        free, count = torch.split_with_sizes(buf, (pages, 1))
+        to = _ptr(buf), _ptr(buf) + 4 * pages
+    else:
+        free, count = out
+        to = _flat(free, "free pages", i32, (pages,)), _flat(count, "count", i32, (1,))
+    fn, name = _entry("ssq_page_collect", torch.bfloat16)
+    _launch(fn, name, lens.device, (table, pinned, free, count, workspace), lp, n, tp, width, page_size, pages, pp, *to, _ptr(workspace),
+            workspace.numel() * workspace.element_size())
+    return free, count
+
+
+def ssq_page_compact(lens: torch.Tensor, table: torch.Tensor, page_size: int, pages: int, pinned: Optional[torch.Tensor] = None,
+                     out=None, workspace: Optional[torch.Tensor] = None):
+    """``ssq_page_collect`` with the held pages brought to the front of the pool: returns (table with the new
+    numbers, free_pages [pages] and count [1] after the moves, src, dst [pages // 2]: the moves, then -1, moved [1]), int32.
+    The moves are to be made in every layer (``ssq_page_copy``) before its cache is next used.  ``out`` = these
+    six reuses buffers; its table may be ``table`` itself."""
+    lp, n, tp, width, pp, workspace = _pool_arguments(lens, table, pages, pinned, 1, workspace)
+    i32, half = torch.int32, pages // 2
+    if out is None:
+        sizes = (n * width, pages, 1, half, half, 1)
+        buf = torch.empty(sum(sizes), dtype=i32, device=lens.device)
+        table_out, free, count, src, dst, moved = torch.split_with_sizes(buf, sizes)
+        table_out = table_out.view(n, width)
+        base = _ptr(buf)
+        to = [base + 4 * sum(sizes[:i]) for i in range(6)]
+    else:
+        table_out, free, count, src, dst, moved = out
+        to = (_flat(table_out, "table out", i32, (n, width)), _flat(free, "free pages", i32, (pages,)), _flat(count, "count", i32, (1,)),
+              _flat(src, "src", i32, (half,)), _flat(dst, "dst", i32, (half,)), _flat(moved, "moved", i32, (1,)))
+    fn, name = _entry("ssq_page_compact", torch.bfloat16)
+    _launch(fn, name, lens.device, (table, pinned, table_out, free, count, src, dst, moved, workspace), lp, n, tp, width, page_size, pages, pp,
+            *to, _ptr(workspace), workspace.numel() * workspace.element_size())
+    return table_out, free, count, src, dst, moved
+
+
+def ssq_page_collect_workspace_size(pages: int, compact: bool = False) -> int:
+    """Bytes of scratch for ssq_page_collect, or (``compact``) for ssq_page_compact."""
+    return int(lib().ssq_page_collect_workspace_size(pages, int(compact)))
+
+
+def ssq_page_copy(caches, src: torch.Tensor, dst: torch.Tensor) -> None:
+    """Page ``src[i]`` of every cache into its page ``dst[i]`` (int32; negative: nothing), on the current stream.
+    ``caches``: contiguous tensors [pages, ...] of one device whose pages have the same number of bytes, such as
+    all layers' k_pages and v_pages, or their 4-bit caches.  No page may be named twice in dst, or in both."""
+    caches = list(caches)
+    if not caches:
+        return
+    shape, size, dev = caches[0].shape, caches[0].element_size(), caches[0].device
+    if not shape or src.dim() != 1:
+        raise ValueError("caches must be [pages, ...], src and dst [entries]")
+    pages, page_bytes = shape[0], shape[1:].numel() * size
+    for c in caches:
+        if c.dim() == 0 or c.shape[0] != pages or c.shape[1:].numel() * c.element_size() != page_bytes or not c.is_contiguous() or c.device != dev:
+            raise ValueError("caches must be contiguous, on one device, and have the same pages and bytes a page")
+    fn, name = _entry("ssq_page_copy", torch.bfloat16)
+    _launch(fn, name, dev, (src, dst), (ctypes.c_void_p * len(caches))(*(_ptr(c) for c in caches)), len(caches), page_bytes, pages,
+            _flat(src, "src", torch.int32, src.shape), _flat(dst, "dst", torch.int32, src.shape), src.shape[0])

@@ -74,22 +74,17 @@ Kv4Plan make_kv4_plan(int64_t requests, int fresh, int q_heads, int kv_heads, in
 template <int D>
 struct Half {
   static constexpr int kGroups = D / 32;
-  uint32_t k[kGroups], v[kGroups];
-  uint32_t k_scale[2 * kGroups], v_scale[2 * kGroups];       // [key][group] in binary16
+  typedef uint32_t Words __attribute__((ext_vector_type(kGroups)));
+  Words k, v;
+  u32x4 k_scale[kGroups / 2], v_scale[kGroups / 2];          // [key][group] in binary16
 };
 
+__device__ __forceinline__ void load_words(__amdgpu_buffer_rsrc_t r, int at, int base, u32x4& w) { w = __builtin_amdgcn_raw_buffer_load_b128(r, at, base, 0); }
+__device__ __forceinline__ void load_words(__amdgpu_buffer_rsrc_t r, int at, int base, u32x2& w) { w = __builtin_amdgcn_raw_buffer_load_b64(r, at, base, 0); }
 template <int N>
-__device__ __forceinline__ void load_words(__amdgpu_buffer_rsrc_t r, int at, int base, uint32_t (&w)[N]) {
+__device__ __forceinline__ void load_words(__amdgpu_buffer_rsrc_t r, int at, int base, u32x4 (&w)[N]) {
 #pragma unroll
-  for (int i = 0; i < N; i += 4) {
-    if constexpr (N % 4 == 0) {
-      const u32x4 d = __builtin_amdgcn_raw_buffer_load_b128(r, at + 4 * i, base, 0);
-      w[i] = d.x, w[i + 1] = d.y, w[i + 2] = d.z, w[i + 3] = d.w;
-    } else {
-      const u32x2 d = __builtin_amdgcn_raw_buffer_load_b64(r, at + 4 * i, base, 0);
-      w[i] = d.x, w[i + 1] = d.y;
-    }
-  }
+  for (int i = 0; i < N; ++i) load_words(r, at + 16 * i, base, w[i]);
 }
 
 __device__ __forceinline__ float max_of_row(float v) {        // of the four lanes that hold a query
@@ -173,15 +168,13 @@ struct Kv4Rows {
       if constexpr (kTerms == 1) start[rt][g] = product(u32x4{kLess136, kLess136, kLess136, kLess136}, q[rt][g][0], start[rt][g]);
     }
     m[rt] = -FLT_MAX;
-    l[rt] = __uint_as_float(kSawNone);
+    l[rt] = 0.0f;
 #pragma unroll
     for (int t = 0; t < 2 * kGroups; ++t) o[rt][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   }
 
-  // The keys of two halves; those that a lane sees of tile rt: bit 4 u + i of seen[rt] for key i of half u.
-  template <bool HIDDEN>
-  __device__ __forceinline__ void take(const Half<D> (&x)[2], float scale, const uint32_t (&seen)[RT]) {
-    f32x4 s[RT][2];
+  // Scores of two halves' keys.
+  __device__ __forceinline__ void score(const Half<D> (&x)[2], f32x4 (&s)[RT][2]) const {
 #pragma unroll
     for (int u = 0; u < 2; ++u)
 #pragma unroll
@@ -194,73 +187,62 @@ struct Kv4Rows {
 #pragma unroll
           for (int n = kTerms - 1; n >= 0; --n) part = product(key, q[rt][g][n], part);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float by = scale_of(x[u].k_scale, i, g);
-            s[rt][u][i] = g == 0 ? part[i] * by : __builtin_fmaf(part[i], by, s[rt][u][i]);
-          }
+          for (int i = 0; i < 4; ++i) s[rt][u][i] = __builtin_fmaf(part[i], scale_of(x[u].k_scale, i, g), g == 0 ? 0.0f : s[rt][u][i]);
         }
       }
-    u32x4 value[2 * kGroups];
+  }
+
+  // The values' codes of two halves, elements 16 t ... 16 t + 15, as an A operand.
+  __device__ __forceinline__ u32x4 value(const Half<D> (&x)[2], int t) const {
+    const uint32_t w[2] = {x[0].v[t / 2], x[1].v[t / 2]};
+    // tokens 0 and 2 of a lane's four, then 1 and 3
+    return u32x4{terms.codes(w[0], t % 2), terms.codes(w[0], t % 2 + 2), terms.codes(w[1], t % 2), terms.codes(w[1], t % 2 + 2)};
+  }
+
+  // What scores of tile rt add: the softmax's step and the product with the values, whose scales x holds.
+  __device__ __forceinline__ void add(int rt, const Half<D> (&x)[2], const f32x4 (&s)[2], float scale) {
+    float most = -INFINITY;
 #pragma unroll
-    for (int t = 0; t < 2 * kGroups; ++t)
+    for (int u = 0; u < 2; ++u)
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const uint32_t w = x[u].v[t / 2];
-        value[t][2 * u] = terms.codes(w, t % 2);          // tokens 0 and 2
-        value[t][2 * u + 1] = terms.codes(w, t % 2 + 2);  // tokens 1 and 3
+      for (int i = 0; i < 4; ++i) most = fmaxf(most, s[u][i]);
+    if (__builtin_amdgcn_ballot_w64(most * scale > m[rt] + kSlack) != 0) move(rt, most * scale);
+    float p[2][4];
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        p[u][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][i], scale, -m[rt]));
+        l[rt] += p[u][i];
       }
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-      float most = -INFINITY;
+    for (int g = 0; g < kGroups; ++g) {
+      u32x4 w[kTerms];
 #pragma unroll
       for (int u = 0; u < 2; ++u)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if (HIDDEN && !(seen[rt] >> (4 * u + i) & 1u)) s[rt][u][i] = -INFINITY;
-          most = fmaxf(most, s[rt][u][i]);
+        for (int i = 0; i < 2; ++i) {
+          uint32_t d[kTerms];
+          // a fused product and sum, whose factors may be binary16 as they are
+          Terms<T>::split(__builtin_fmaf(p[u][i], scale_of(x[u].v_scale, i, g), 0.0f), __builtin_fmaf(p[u][i + 2], scale_of(x[u].v_scale, i + 2, g), 0.0f), d);
+#pragma unroll
+          for (int n = 0; n < kTerms; ++n) w[n][2 * u + i] = d[n];
         }
-      if (__builtin_amdgcn_ballot_w64(most * scale > m[rt] + kSlack) != 0) move(rt, most * scale);
-      float p[2][4];
+      const u32x4 values[2] = {value(x, 2 * g), value(x, 2 * g + 1)};
 #pragma unroll
-      for (int u = 0; u < 2; ++u)
+      for (int n = kTerms - 1; n >= 0; --n)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          p[u][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rt][u][i], scale, -m[rt]));
-          if (HIDDEN && !(seen[rt] >> (4 * u + i) & 1u)) p[u][i] = __uint_as_float(kSawNone);
-          l[rt] += p[u][i];
-        }
+        for (int e = 0; e < 2; ++e) o[rt][2 * g + e] = product(values[e], w[n], o[rt][2 * g + e]);
+      if constexpr (kTerms == 1)
 #pragma unroll
-      for (int g = 0; g < kGroups; ++g) {
-        u32x4 w[kTerms];
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            uint32_t d[kTerms];
-            float by[2];
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              by[e] = scale_of(x[u].v_scale, i + 2 * e, g);
-              if (HIDDEN && !(seen[rt] >> (4 * u + i + 2 * e) & 1u)) by[e] = 0.0f;
-            }
-            Terms<T>::split(p[u][i] * by[0], p[u][i + 2] * by[1], d);
-#pragma unroll
-            for (int n = 0; n < kTerms; ++n) w[n][2 * u + i] = d[n];
-          }
-#pragma unroll
-        for (int n = kTerms - 1; n >= 0; --n)
-#pragma unroll
-          for (int e = 0; e < 2; ++e) o[rt][2 * g + e] = product(value[2 * g + e], w[n], o[rt][2 * g + e]);
-        if constexpr (kTerms == 1)
-#pragma unroll
-          for (int e = 0; e < 2; ++e) o[rt][2 * g + e] = product(u32x4{kLess136, kLess136, kLess136, kLess136}, w[0], o[rt][2 * g + e]);
-      }
+        for (int e = 0; e < 2; ++e) o[rt][2 * g + e] = product(u32x4{kLess136, kLess136, kLess136, kLess136}, w[0], o[rt][2 * g + e]);
     }
   }
 
-  static __device__ __forceinline__ float scale_of(const uint32_t (&w)[2 * kGroups], int key, int g) {
+  static __device__ __forceinline__ float scale_of(const u32x4 (&w)[kGroups / 2], int key, int g) {
     const int at = key * kGroups + g;
-    return at % 2 == 0 ? f16_lo(w[at / 2]) : f16_hi(w[at / 2]);
+    const uint32_t pair = w[at / 8][at / 2 % 4];
+    return at % 2 == 0 ? f16_lo(pair) : f16_hi(pair);
   }
 
   // The references of rows whose maximum is more than kSlack above them, from the lanes' own maxima.
@@ -288,7 +270,7 @@ template <typename T, int D, int RT>
 __device__ __forceinline__ void walk_rows(const Decode<T>& a, const uint8_t* cache, const Kv4Plan& p, const Parts& parts, int head, int request,
                                           int index0, const KeyRange (&range)[2], int part, float* lds, float2 (*ml)[RT * kRows]) {
   constexpr int kGroups = D / 32;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane / 16, x = lane & 15;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane / 16, col = lane & 15;
   const int rows = request < 0 ? p.rows : a.fresh * p.group;
   auto find_row = [&](int n) {
     Row row;
@@ -304,7 +286,7 @@ __device__ __forceinline__ void walk_rows(const Decode<T>& a, const uint8_t* cac
   int last[RT], first_last = 0x7fffffff;
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
-    const Row row = find_row(rt * kRows + x);
+    const Row row = find_row(rt * kRows + col);
     last[rt] = row.last;
     if (row.present) first_last = min(first_last, row.last);
     r.load_query(rt, a.q.p + row.line * a.q.stride + row.column * D, row.present, h);
@@ -312,12 +294,12 @@ __device__ __forceinline__ void walk_rows(const Decode<T>& a, const uint8_t* cac
   const int wave_first = wave_min(first_last);
   const float scale = a.scale * kLog2e;
   const int shift = a.cache.page_shift, in_page = (1 << shift) - 1, part_bytes = Kv4<D>::part(shift);
-  const int k_at = x * Kv4<D>::kCodes + h * 4 * kGroups, v_at = lane * 4 * kGroups, scale_at = h * 4 * Kv4<D>::kScales;
+  const int k_at = col * Kv4<D>::kCodes + h * 4 * kGroups, v_at = lane * 4 * kGroups, scale_at = h * 4 * Kv4<D>::kScales;
   const int tiles0 = range[0].tiles(), tiles = tiles0 + range[1].tiles();
 
   struct Place {                          // a tile's halves: first key, and the pages they lie in (-1: absent)
     int first, begin, end;
-    int64_t page[2];
+    int32_t page[2];
   };
   auto place = [&](int t) {
     Place at = {0, 0, 0, {-1, -1}};
@@ -336,49 +318,87 @@ __device__ __forceinline__ void walk_rows(const Decode<T>& a, const uint8_t* cac
     }
     return at;
   };
-  auto load = [&](Half<D> (&to)[2], const Place& at) {
+  auto record = [&](const Place& at, int u) {
+    const bool here = at.page[u] >= 0;
+    return make_rsrc(cache + ((here ? at.page[u] : 0) * (int64_t)a.kv_heads + head) * (int64_t)(2 * part_bytes), here ? 2 * part_bytes : 0);
+  };
+  Half<D> x[2];
+  auto load_keys = [&](const Place& at) {
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      const bool here = at.page[u] >= 0;
-      const uint8_t* base = cache + ((here ? at.page[u] : 0) * a.kv_heads + head) * (int64_t)(2 * part_bytes);
-      const __amdgpu_buffer_rsrc_t rsrc = make_rsrc(base, here ? 2 * part_bytes : 0);
-      const int t0 = (at.first + 16 * u) & in_page, codes = t0 * Kv4<D>::kCodes, scales = (Kv4<D>::kCodes << shift) + t0 * Kv4<D>::kScales;
-      load_words(rsrc, k_at, codes, to[u].k);
-      load_words(rsrc, scale_at, scales, to[u].k_scale);
-      load_words(rsrc, v_at, part_bytes + codes, to[u].v);
-      load_words(rsrc, scale_at, part_bytes + scales, to[u].v_scale);
+      const __amdgpu_buffer_rsrc_t rsrc = record(at, u);
+      const int t0 = (at.first + 16 * u) & in_page;
+      load_words(rsrc, k_at, t0 * Kv4<D>::kCodes, x[u].k);
+      load_words(rsrc, scale_at, (Kv4<D>::kCodes << shift) + t0 * Kv4<D>::kScales, x[u].k_scale);
     }
   };
-  auto take = [&](const Half<D> (&of)[2], const Place& at) {
-    uint32_t seen[RT];
-    const bool whole = at.first >= at.begin && at.first + kTileKeys - 1 <= min(wave_first, at.end - 1) && at.page[0] >= 0 && at.page[1] >= 0;
-    if (whole) return r.template take<false>(of, scale, seen);
+  auto load_value_scales = [&](const Place& at) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+      load_words(record(at, u), scale_at, part_bytes + (Kv4<D>::kCodes << shift) + ((at.first + 16 * u) & in_page) * Kv4<D>::kScales, x[u].v_scale);
+  };
+  auto load_values = [&](const Place& at) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) load_words(record(at, u), v_at, part_bytes + ((at.first + 16 * u) & in_page) * Kv4<D>::kCodes, x[u].v);
+    load_value_scales(at);
+  };
+  uint32_t saw[RT] = {};                  // whether a lane has seen a key
+  bool all_saw = false;                   // a tile of which every row sees every key
+  Place at = place(wave), then = place(wave + kWaves);
+  if (wave < tiles) {
+    load_keys(at);
+    load_values(at);
+  }
+#pragma unroll 1
+  for (int t = wave; t < tiles; t += kWaves) {
+    const Place later = place(t + 2 * kWaves);
+    const bool whole = ((at.first >= at.begin) & (at.first + kTileKeys - 1 <= min(wave_first, at.end - 1)) & ((at.page[0] | at.page[1]) >= 0)) != 0;
+    all_saw |= whole;
+    f32x4 s[RT][2];
+    r.score(x, s);
+    // the next keys take these ones' registers: all that reads them stays before the loads
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+      for (int u = 0; u < 2; ++u) asm volatile("" : "+v"(s[rt][u]));
+    __builtin_amdgcn_sched_barrier(0);
+    load_keys(then);
+    __builtin_amdgcn_sched_barrier(0);
+    uint32_t seen[RT] = {};               // bit 4 u + i: whether a lane sees key i of its four of half u
+    if (!whole) {
+      asm volatile("");                   // a branch, not selects in every tile
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int j = at.first + 16 * u + 4 * h + i;
+            const bool sees = at.page[u] >= 0 && j >= at.begin && j <= min(last[rt], at.end - 1);
+            s[rt][u][i] = sees ? s[rt][u][i] : -INFINITY;
+            seen[rt] |= sees ? 1u << (4 * u + i) : 0u;
+          }
+    }
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-      seen[rt] = 0;
+      if (!whole) {                       // the scales of keys that tile rt's rows do not see
+        if (rt > 0) load_value_scales(at);
+        saw[rt] |= seen[rt];
 #pragma unroll
-      for (int u = 0; u < 2; ++u)
+        for (int u = 0; u < 2; ++u)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int j = at.first + 16 * u + 4 * h + i;
-          if (at.page[u] >= 0 && j >= at.begin && j <= min(last[rt], at.end - 1)) seen[rt] |= 1u << (4 * u + i);
-        }
+          for (int n = 0; n < kGroups / 2; ++n) {           // 8 / kGroups keys each
+            u32x4 keep;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) keep[i] = 0u - (seen[rt] >> (4 * u + (8 * n + 2 * i) / kGroups) & 1u);
+            x[u].v_scale[n] &= keep;
+          }
+      }
+      r.add(rt, x, s[rt], scale);
     }
-    r.template take<true>(of, scale, seen);
-  };
-  Half<D> now[2], next[2];
-  Place at = place(wave), then = place(wave + kWaves);
-  if (wave < tiles) load(now, at);
-#pragma unroll 1
-  for (int t = wave; t < tiles; t += 2 * kWaves) {
-    Place later = place(t + 2 * kWaves);
-    load(next, then);
-    take(now, at);
-    if (t + kWaves >= tiles) break;
-    at = later;
-    later = place(t + 3 * kWaves);
-    load(now, at);
-    take(next, then);
+    __builtin_amdgcn_sched_barrier(0);
+    load_values(then);
+    at = then;
     then = later;
   }
 
@@ -386,11 +406,12 @@ __device__ __forceinline__ void walk_rows(const Decode<T>& a, const uint8_t* cac
   constexpr int kPitch = D + 4;
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
-    const float l = sum_of_row(r.l[rt]);
-    if (h == 0) ml[wave][rt * kRows + x] = float2{r.m[rt], l};
+    const bool saw_one = all_saw || max_of_row((float)saw[rt]) != 0.0f;
+    const float l = saw_one ? sum_of_row(r.l[rt]) : __uint_as_float(kSawNone);
+    if (h == 0) ml[wave][rt * kRows + col] = float2{r.m[rt], l};
 #pragma unroll
     for (int t = 0; t < 2 * kGroups; ++t)
-      *reinterpret_cast<f32x4*>(lds + (wave * RT * kRows + rt * kRows + x) * kPitch + 16 * t + 4 * h) = r.o[rt][t];
+      *reinterpret_cast<f32x4*>(lds + (wave * RT * kRows + rt * kRows + col) * kPitch + 16 * t + 4 * h) = r.o[rt][t];
   }
   __syncthreads();
   constexpr int kChunks = D / 4;
@@ -418,7 +439,7 @@ __device__ __forceinline__ void walk_rows(const Decode<T>& a, const uint8_t* cac
 }
 
 template <typename T, int D, int RT>
-__global__ __launch_bounds__(kThreads, 2) void decode_kv4_kernel(const Decode<T> a, const uint8_t* cache, const Kv4Plan p, const Parts parts, int prefix_groups, bool sorted) {
+__global__ __launch_bounds__(kThreads, sizeof(T) == 2 && RT == 1 ? 3 : 2) void decode_kv4_kernel(const Decode<T> a, const uint8_t* cache, const Kv4Plan p, const Parts parts, int prefix_groups, bool sorted) {
   __shared__ __align__(16) float lds[kWaves * RT * kRows * (D + 4)];
   __shared__ float2 ml[kWaves][RT * kRows];
   const int prefix = (int)min(a.prefix, min(a.max_len, a.table_stride << a.cache.page_shift));

@@ -26,12 +26,14 @@ namespace ssq {
 namespace attention {
 namespace {
 
-constexpr int kWaves = 4, kThreads = 64 * kWaves, kRows = 16, kTileKeys = 32;
+constexpr int kWaves = 4, kThreads = 64 * kWaves, kTileKeys = 32;
 constexpr int kStepKeys = kTileKeys * kWaves;         // keys that a workgroup takes at a time
+constexpr int kWideRows = 32;                         // rows of a workgroup where they are many (two tiles of 16)
 
 struct Kv4Plan {
   int group;             // query heads of a key/value head
   int rows;              // requests * fresh * group: rows of a key/value head
+  int own_rows;          // rows of a workgroup on a request's own keys: 4, 8, 16 or 32
   bool share;            // whether the prefix is taken for all requests at once
   int prefix_tiles, prefix_parts;
   int own_tiles, own_parts;
@@ -40,52 +42,145 @@ struct Kv4Plan {
   int64_t prefix_groups() const { return share ? (int64_t)prefix_tiles * prefix_parts : 0; }
 };
 
+constexpr int kPartCounts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};      // that are looked at
+static_assert(kPartCounts[sizeof(kPartCounts) / sizeof(int) - 1] == kMaxParts);
+int64_t steps_of(int64_t keys, int parts) { return ceil_div(ceil_div(keys, parts), kStepKeys); }
 
+// Parts of the requests' own keys where no prefix is shared, for `groups` workgroups a part: the quickest by a fit
+// of its time (us).  A step of 128 keys takes a workgroup 1.1 where it has a CU to itself, two beside each other
+// 1.8, three 2.35, and a CU full of them 0.8 each; parts have to be joined, by a launch of 3 and their traffic.  1 request of 16383 keys (8
+// key/value heads): 32 parts 12.3 us, 16 15.0, 64 13.7; 16 of 1024: 1 part 12.3, 4 parts 12.2, 8 parts 13.1; 32 of
+// 4096: 1 part 42.0, 2 parts 38.2, 3 parts 35.2, 8 parts 39.5; 48 of 4096 to 8191: 1 part 101, 2 parts 73, 4 parts 78; 64 of 1024:
+// 1 part 16.6, 2 parts 20.7.
+int choose_parts(int64_t groups, int64_t keys, int64_t line_rows) {
+  int best = 1;
+  double best_us = 0.0;
+  for (const int n : kPartCounts) {
+    if (n > 1 && (n - 1) * kStepKeys >= keys) break;
+    const int64_t beside = ceil_div(groups * n, 256);
+    const double step_us = beside == 1 ? 1.1 : beside == 2 ? 1.8 : beside == 3 ? 2.35 : 0.8 * (double)beside;
+    const double us = step_us * (double)steps_of(keys, n) + (n > 1 ? 3.0 : 0.0) + n * (0.04 + 0.6e-3 * (double)line_rows);
+    if (n == 1 || us < best_us) best = n, best_us = us;
+  }
+  return best;
+}
 
+// The same beside a prefix, whose workgroups take 1.3 for a step of 128 keys and 32 rows, 2.3 where a CU has two of
+// them, and in between where it has work on own keys too; a CU that is full does a step in 1.15, one of a
+// request's own keys in 0.8.  Together: the work, or the longest workgroup.  64 requests of one key behind 8192 (256 rows, 8 key/value heads): 4 parts 32.3 us, 8 parts 32.8, 16
+// parts 40.0; behind 16384: 50.8, 45.0, 52.4; of 1 to 1024 keys behind 8192: 34.8 with 4 parts and 1, 40.6 with 3
+// and 1, 40.8 with 8 and 1.
+void choose_shared_parts(Kv4Plan& p, int64_t requests, int kv_heads, int64_t prefix, int64_t behind) {
+  const int64_t wide = (int64_t)p.prefix_tiles * kv_heads, own = requests * p.own_tiles * kv_heads;
+  double best_us = 0.0;
+  for (const int n : kPartCounts) {
+    if (n > kMaxParts / 2 || (n > 1 && (n - 1) * kStepKeys >= prefix)) break;
+    for (const int m : {1, 2, 4, 8}) {
+      if (m > 1 && (m - 1) * kStepKeys >= behind) break;
+      const double wide_steps = (double)steps_of(prefix, n), own_steps = (double)steps_of(behind, m);
+      const double wide_us = 1.15 * wide_steps * (double)(wide * n) / 256.0, own_us = 0.8 * own_steps * (double)(own * m) / 256.0;
+      const double pace = wide * n > 256 ? 2.3 : 1.3 + 0.6 * std::min(1.0, own_us / wide_us), all = wide_us + own_us;
+      const double longest = std::max(wide_steps * pace, own_steps * 1.5);
+      const double us = std::max(all, longest) + 0.5e-3 * (double)((n + m) * p.line_rows);
+      if ((n == 1 && m == 1) || us < best_us) p.prefix_parts = n, p.own_parts = m, best_us = us;
+    }
+  }
+}
 
-Kv4Plan make_kv4_plan(int64_t requests, int fresh, int q_heads, int kv_heads, int64_t max_len, int64_t prefix, bool split) {
+Kv4Plan make_kv4_plan(int64_t requests, int fresh, int q_heads, int kv_heads, int head_dim, int64_t max_len, int64_t prefix, bool split) {
   Kv4Plan p = {};
   p.group = q_heads / kv_heads;
   p.rows = (int)(requests * fresh * p.group);
   p.line_rows = requests * fresh * q_heads;
-  p.own_tiles = (int)ceil_div((int64_t)fresh * p.group, kRows);
+  const int64_t mine = (int64_t)fresh * p.group;
+  p.own_rows = mine <= 4 && head_dim == 128 ? 4 : mine <= 8 ? 8 : mine <= 16 ? 16 : kWideRows;
+  p.own_tiles = (int)ceil_div(mine, p.own_rows);
   p.own_parts = 1;
   if (!split) return p;
-  constexpr int64_t kGroups = 512;       // two workgroups for each of 256 CUs
   prefix = std::min(prefix, max_len);
   if (requests > 1 && prefix > 0) {
     p.share = true;
-    p.prefix_tiles = (int)ceil_div(p.rows, kRows);
-    p.prefix_parts = (int)std::clamp(ceil_div(kGroups, (int64_t)p.prefix_tiles * kv_heads), (int64_t)1,
-                                     std::min<int64_t>(kMaxParts / 2, ceil_div(prefix, 2 * kStepKeys)));
+    p.prefix_tiles = (int)ceil_div(p.rows, kWideRows);
+    choose_shared_parts(p, requests, kv_heads, prefix, max_len - prefix);
   } else {
-    prefix = 0;
+    p.own_parts = choose_parts(requests * kv_heads * p.own_tiles, max_len, p.line_rows);
   }
-  const int64_t behind = max_len - prefix, groups = requests * kv_heads * p.own_tiles;
-  p.own_parts = (int)std::clamp(ceil_div(kGroups, groups), (int64_t)1,
-                                std::min<int64_t>(kMaxParts / 2, std::max<int64_t>(1, ceil_div(behind, 2 * kStepKeys))));
   // nothing is shared or split where a launch could not hold it: own_tiles alone fit one (checked before)
   if ((p.prefix_groups() + requests * p.own_tiles * p.own_parts) * kv_heads >= kMaxGroups || p.line_rows >= kJoinThreads / 64 * kMaxGroups)
-    return make_kv4_plan(requests, fresh, q_heads, kv_heads, max_len, 0, false);
+    return make_kv4_plan(requests, fresh, q_heads, kv_heads, head_dim, max_len, 0, false);
   return p;
 }
 
-// What a lane loads of 16 keys and their values: the words of kv4.h, and the scales of four keys.
+// F column groups share a product's 16 columns: with few rows, column cg * (16 / F) + i of it is query i against the
+// head's groups cg * kSets ... cg * kSets + kSets - 1 alone (its operands are zero for the others).  So a chain of F
+// products leaves F groups' sums in one accumulator, each lane scales its own groups only, and the columns are
+// added up once they are scores; the weights are scaled likewise, and of an output tile the columns of its
+// own group count.
+template <int D, int F>
+struct Fold {
+  static constexpr int kGroups = D / 32, kSets = kGroups / F, kRows = 16 / F;
+  static_assert(kGroups % F == 0 && (F == 1 || kSets <= 2), "a lane's groups share a word of scales");
+};
+
+// The scales of four keys, for the groups of a lane: binary16, where `of` finds them.
+template <int D, int F>
+struct Spread {
+  using S = Fold<D, F>;
+  u32x4 w[F == 1 ? S::kGroups / 2 : 1];          // [key][group]; folded: a word a key
+  __device__ __forceinline__ float of(int key, int set) const {
+    const int at = F == 1 ? key * S::kGroups + set : 2 * key + set;
+    const uint32_t pair = w[at / 8][at / 2 % 4];
+    return at % 2 == 0 ? f16_lo(pair) : f16_hi(pair);
+  }
+  // Zeros for keys without their bit in `seen`.
+  __device__ __forceinline__ void keep(uint32_t seen) {
+#pragma unroll
+    for (int n = 0; n < (int)(sizeof(w) / sizeof(w[0])); ++n) {
+      u32x4 mask;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) mask[i] = 0u - (seen >> (F == 1 ? (8 * n + 2 * i) / S::kGroups : i) & 1u);
+      w[n] &= mask;
+    }
+  }
+};
+
+// As they are loaded.  Folded, a lane loads the word of one key of its four, which the four lanes side by side exchange.
+template <int D, int F>
+struct Scales {
+  uint32_t w;
+  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t r, int at, int base) {
+    if constexpr (Fold<D, F>::kSets == 1) w = __builtin_amdgcn_raw_buffer_load_b16(r, at, base, 0);
+    else w = __builtin_amdgcn_raw_buffer_load_b32(r, at, base, 0);
+  }
+  static __device__ __forceinline__ int lane_at(int h, int col) {
+    return (4 * h + (col & 3)) * Kv4<D>::kScales + col / Fold<D, F>::kRows * 2 * Fold<D, F>::kSets;
+  }
+  template <int KEY>
+  __device__ __forceinline__ uint32_t of_key() const { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)w, 0x55 * KEY, 0xF, 0xF, true); }
+  __device__ __forceinline__ Spread<D, F> spread() const { return {{u32x4{of_key<0>(), of_key<1>(), of_key<2>(), of_key<3>()}}}; }
+};
 template <int D>
+struct Scales<D, 1> {
+  Spread<D, 1> all;
+  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t r, int at, int base) {
+#pragma unroll
+    for (int n = 0; n < D / 64; ++n) all.w[n] = __builtin_amdgcn_raw_buffer_load_b128(r, at + 16 * n, base, 0);
+  }
+  static __device__ __forceinline__ int lane_at(int h, int) { return 4 * h * Kv4<D>::kScales; }
+  __device__ __forceinline__ Spread<D, 1> spread() const { return all; }
+};
+
+// What a lane loads of 16 keys and their values: the words of kv4.h, and scales.
+template <int D, int F>
 struct Half {
   static constexpr int kGroups = D / 32;
   typedef uint32_t Words __attribute__((ext_vector_type(kGroups)));
   Words k, v;
-  u32x4 k_scale[kGroups / 2], v_scale[kGroups / 2];          // [key][group] in binary16
+  Scales<D, F> k_scale, v_scale;
 };
 
 __device__ __forceinline__ void load_words(__amdgpu_buffer_rsrc_t r, int at, int base, u32x4& w) { w = __builtin_amdgcn_raw_buffer_load_b128(r, at, base, 0); }
 __device__ __forceinline__ void load_words(__amdgpu_buffer_rsrc_t r, int at, int base, u32x2& w) { w = __builtin_amdgcn_raw_buffer_load_b64(r, at, base, 0); }
-template <int N>
-__device__ __forceinline__ void load_words(__amdgpu_buffer_rsrc_t r, int at, int base, u32x4 (&w)[N]) {
-#pragma unroll
-  for (int i = 0; i < N; ++i) load_words(r, at + 16 * i, base, w[i]);
-}
 
 __device__ __forceinline__ float max_of_row(float v) {        // of the four lanes that hold a query
   const auto s = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
@@ -148,24 +243,27 @@ struct Terms<float> {
   }
 };
 
-// RT tiles of 16 query rows of a wavefront.
-template <typename T, int D, int RT>
+// RT tiles of 16 / F query rows of a wavefront.
+template <typename T, int D, int RT, int F>
 struct Kv4Rows {
-  static constexpr int kGroups = D / 32, kTerms = Terms<T>::kCount;
+  using S = Fold<D, F>;
+  static constexpr int kGroups = S::kGroups, kSets = S::kSets, kTerms = Terms<T>::kCount;
+  static constexpr bool kOffset = kTerms == 1;         // whether codes enter with 136 too many
   Terms<T> terms;
   u32x4 q[RT][kGroups][kTerms];
-  f32x4 start[RT][kGroups];              // -136 times the sum of the group's elements, in bf16
-  f32x4 o[RT][2 * kGroups];              // element 16 t + 4 h + i of query x, in tile t's register i
+  f32x4 start[RT][kSets];                // -136 times the sum of the groups' elements
+  f32x4 o[RT][2 * kGroups];              // element 16 t + 4 h + i of the column's query, in tile t's register i
   float m[RT], l[RT];
 
-  __device__ __forceinline__ void load_query(int rt, const T* row, bool present, int h) {
+  __device__ __forceinline__ void load_query(int rt, const T* row, bool present, int h, int col) {
+#pragma unroll
+    for (int j = 0; j < kSets; ++j) start[rt][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int g = 0; g < kGroups; ++g) {
 #pragma unroll
       for (int n = 0; n < kTerms; ++n) q[rt][g][n] = u32x4{0u, 0u, 0u, 0u};
-      if (present) Terms<T>::query(row + 32 * g + 8 * h, q[rt][g]);
-      start[rt][g] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-      if constexpr (kTerms == 1) start[rt][g] = product(u32x4{kLess136, kLess136, kLess136, kLess136}, q[rt][g][0], start[rt][g]);
+      if (present && col / S::kRows == g / kSets) Terms<T>::query(row + 32 * g + 8 * h, q[rt][g]);
+      if constexpr (kOffset) start[rt][g % kSets] = product(u32x4{kLess136, kLess136, kLess136, kLess136}, q[rt][g][0], start[rt][g % kSets]);
     }
     m[rt] = -FLT_MAX;
     l[rt] = 0.0f;
@@ -174,33 +272,56 @@ struct Kv4Rows {
   }
 
   // Scores of two halves' keys.
-  __device__ __forceinline__ void score(const Half<D> (&x)[2], f32x4 (&s)[RT][2]) const {
+  __device__ __forceinline__ void score(const Half<D, F> (&x)[2], f32x4 (&s)[RT][2]) const {
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
+    for (int u = 0; u < 2; ++u) {
+      const Spread<D, F> by = x[u].k_scale.spread();
 #pragma unroll
-      for (int g = 0; g < kGroups; ++g) {
-        const uint32_t w = x[u].k[g];
-        const u32x4 key = {terms.codes(w, 0), terms.codes(w, 1), terms.codes(w, 2), terms.codes(w, 3)};
+      for (int j = 0; j < kSets; ++j) {
+        f32x4 part[RT];
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt) {
-          f32x4 part = start[rt][g];
+        for (int rt = 0; rt < RT; ++rt) part[rt] = start[rt][j];
 #pragma unroll
-          for (int n = kTerms - 1; n >= 0; --n) part = product(key, q[rt][g][n], part);
+        for (int g = j; g < kGroups; g += kSets) {
+          const uint32_t w = x[u].k[g];
+          const u32x4 key = {terms.codes(w, 0), terms.codes(w, 1), terms.codes(w, 2), terms.codes(w, 3)};
 #pragma unroll
-          for (int i = 0; i < 4; ++i) s[rt][u][i] = __builtin_fmaf(part[i], scale_of(x[u].k_scale, i, g), g == 0 ? 0.0f : s[rt][u][i]);
+          for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+            for (int n = kTerms - 1; n >= 0; --n) part[rt] = product(key, q[rt][g][n], part[rt]);
         }
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) s[rt][u][i] = __builtin_fmaf(part[rt][i], by.of(i, j), j == 0 ? 0.0f : s[rt][u][i]);
       }
+      if constexpr (F > 1) {               // over the column groups; every column has the sum
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            s[rt][u][i] += turned<8>(s[rt][u][i]);
+            if constexpr (F == 4) s[rt][u][i] += turned<4>(s[rt][u][i]);
+          }
+      }
+    }
+  }
+
+  // The value N columns further, round the 16.
+  template <int N>
+  static __device__ __forceinline__ float turned(float v) {
+    return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), 0x120 + N, 0xF, 0xF, true));
   }
 
   // The values' codes of two halves, elements 16 t ... 16 t + 15, as an A operand.
-  __device__ __forceinline__ u32x4 value(const Half<D> (&x)[2], int t) const {
+  __device__ __forceinline__ u32x4 value(const Half<D, F> (&x)[2], int t) const {
     const uint32_t w[2] = {x[0].v[t / 2], x[1].v[t / 2]};
     // tokens 0 and 2 of a lane's four, then 1 and 3
     return u32x4{terms.codes(w[0], t % 2), terms.codes(w[0], t % 2 + 2), terms.codes(w[1], t % 2), terms.codes(w[1], t % 2 + 2)};
   }
 
-  // What scores of tile rt add: the softmax's step and the product with the values, whose scales x holds.
-  __device__ __forceinline__ void add(int rt, const Half<D> (&x)[2], const f32x4 (&s)[2], float scale) {
+  // What scores of tile rt add: the softmax's step and the product with the values.
+  __device__ __forceinline__ void add(int rt, const Half<D, F> (&x)[2], const Spread<D, F> (&by)[2], const f32x4 (&s)[2], float scale) {
     float most = -INFINITY;
 #pragma unroll
     for (int u = 0; u < 2; ++u)
@@ -216,7 +337,7 @@ struct Kv4Rows {
         l[rt] += p[u][i];
       }
 #pragma unroll
-    for (int g = 0; g < kGroups; ++g) {
+    for (int j = 0; j < kSets; ++j) {
       u32x4 w[kTerms];
 #pragma unroll
       for (int u = 0; u < 2; ++u)
@@ -224,25 +345,22 @@ struct Kv4Rows {
         for (int i = 0; i < 2; ++i) {
           uint32_t d[kTerms];
           // a fused product and sum, whose factors may be binary16 as they are
-          Terms<T>::split(__builtin_fmaf(p[u][i], scale_of(x[u].v_scale, i, g), 0.0f), __builtin_fmaf(p[u][i + 2], scale_of(x[u].v_scale, i + 2, g), 0.0f), d);
+          Terms<T>::split(__builtin_fmaf(p[u][i], by[u].of(i, j), 0.0f), __builtin_fmaf(p[u][i + 2], by[u].of(i + 2, j), 0.0f), d);
 #pragma unroll
           for (int n = 0; n < kTerms; ++n) w[n][2 * u + i] = d[n];
         }
-      const u32x4 values[2] = {value(x, 2 * g), value(x, 2 * g + 1)};
 #pragma unroll
-      for (int n = kTerms - 1; n >= 0; --n)
+      for (int g = j; g < kGroups; g += kSets) {
+        const u32x4 values[2] = {value(x, 2 * g), value(x, 2 * g + 1)};
 #pragma unroll
-        for (int e = 0; e < 2; ++e) o[rt][2 * g + e] = product(values[e], w[n], o[rt][2 * g + e]);
-      if constexpr (kTerms == 1)
+        for (int n = kTerms - 1; n >= 0; --n)
 #pragma unroll
-        for (int e = 0; e < 2; ++e) o[rt][2 * g + e] = product(u32x4{kLess136, kLess136, kLess136, kLess136}, w[0], o[rt][2 * g + e]);
+          for (int e = 0; e < 2; ++e) o[rt][2 * g + e] = product(values[e], w[n], o[rt][2 * g + e]);
+        if constexpr (kOffset)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) o[rt][2 * g + e] = product(u32x4{kLess136, kLess136, kLess136, kLess136}, w[0], o[rt][2 * g + e]);
+      }
     }
-  }
-
-  static __device__ __forceinline__ float scale_of(const u32x4 (&w)[kGroups / 2], int key, int g) {
-    const int at = key * kGroups + g;
-    const uint32_t pair = w[at / 8][at / 2 % 4];
-    return at % 2 == 0 ? f16_lo(pair) : f16_hi(pair);
   }
 
   // The references of rows whose maximum is more than kSlack above them, from the lanes' own maxima.
@@ -265,11 +383,20 @@ struct KeyRange {
   __device__ __forceinline__ int tiles() const { return end > begin ? (end - (begin & ~15) + kTileKeys - 1) / kTileKeys : 0; }
 };
 
-// Up to RT tiles of rows from index0 on, of `request` (of all requests if it is negative), against two ranges.
-template <typename T, int D, int RT>
+// What a workgroup's wavefronts leave in LDS, of ROWS rows.
+template <int D, int ROWS>
+struct Shared {
+  static constexpr int kPitch = D + 4;
+  float o[kWaves][ROWS][kPitch];
+  float2 ml[kWaves][ROWS];
+};
+
+// Up to RT * 16 / F rows from index0 on, of `request` (of all requests if it is negative), against two ranges.
+template <typename T, int D, int RT, int F>
 __device__ __forceinline__ void walk_rows(const Decode<T>& a, const uint8_t* cache, const Kv4Plan& p, const Parts& parts, int head, int request,
-                                          int index0, const KeyRange (&range)[2], int part, float* lds, float2 (*ml)[RT * kRows]) {
-  constexpr int kGroups = D / 32;
+                                          int index0, const KeyRange (&range)[2], int part, Shared<D, RT * 16 / F>& lds) {
+  using S = Fold<D, F>;
+  constexpr int kGroups = S::kGroups, kRows = RT * S::kRows;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane / 16, col = lane & 15;
   const int rows = request < 0 ? p.rows : a.fresh * p.group;
   auto find_row = [&](int n) {
@@ -282,77 +409,91 @@ __device__ __forceinline__ void walk_rows(const Decode<T>& a, const uint8_t* cac
     row.last = row.present ? request_len(a, of) - a.fresh + (int)(row.line - (int64_t)of * a.fresh) : -1;
     return row;
   };
-  Kv4Rows<T, D, RT> r;
+  Kv4Rows<T, D, RT, F> r;
   int last[RT], first_last = 0x7fffffff;
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
-    const Row row = find_row(rt * kRows + col);
+    const Row row = find_row(rt * S::kRows + col % S::kRows);
     last[rt] = row.last;
     if (row.present) first_last = min(first_last, row.last);
-    r.load_query(rt, a.q.p + row.line * a.q.stride + row.column * D, row.present, h);
+    r.load_query(rt, a.q.p + row.line * a.q.stride + row.column * D, row.present, h, col);
   }
   const int wave_first = wave_min(first_last);
   const float scale = a.scale * kLog2e;
-  const int shift = a.cache.page_shift, in_page = (1 << shift) - 1, part_bytes = Kv4<D>::part(shift);
-  const int k_at = col * Kv4<D>::kCodes + h * 4 * kGroups, v_at = lane * 4 * kGroups, scale_at = h * 4 * Kv4<D>::kScales;
-  const int tiles0 = range[0].tiles(), tiles = tiles0 + range[1].tiles();
+  const int shift = a.cache.page_shift, in_page = (1 << shift) - 1, part_bytes = Kv4<D>::part(shift), scales = Kv4<D>::kCodes << shift;
+  const int k_at = col * Kv4<D>::kCodes + h * 4 * kGroups, v_at = lane * 4 * kGroups, scale_at = Scales<D, F>::lane_at(h, col);
+  const uint8_t* of_head = cache + head * (int64_t)(2 * part_bytes);
+  const int64_t page_bytes = (int64_t)a.kv_heads * (2 * part_bytes);
+  const int tiles0 = range[0].tiles(), tiles = tiles0 + range[1].tiles(), first0 = range[0].begin & ~15, first1 = range[1].begin & ~15;
 
-  struct Place {                          // a tile's halves: first key, and the pages they lie in (-1: absent)
+  struct Place {                          // a tile: its first key, its range's ends, and the table's entries for its halves
     int first, begin, end;
     int32_t page[2];
   };
-  auto place = [&](int t) {
-    Place at = {0, 0, 0, {-1, -1}};
-    if (t >= tiles) return at;
-    const bool one = t >= tiles0;
-    const KeyRange& of = one ? range[1] : range[0];
-    at.begin = of.begin, at.end = of.end;
-    at.first = (of.begin & ~15) + kTileKeys * (one ? t - tiles0 : t);
+  auto place = [&](int t) {               // entries are looked at a tile later: nothing waits for them here
+    Place at;
+    const int of = min(t, tiles - 1);     // behind the last tile its entries again, and no keys
+    const bool one = of >= tiles0;
+    at.first = one ? first1 + kTileKeys * (of - tiles0) : first0 + kTileKeys * of;
+    at.begin = one ? range[1].begin : range[0].begin;
+    const int end = one ? range[1].end : range[0].end;
+    at.end = t < tiles ? end : 0;
     typedef const __attribute__((address_space(4))) int32_t* uniform_ptr;
+    const uniform_ptr row = (uniform_ptr)(one ? range[1].row : range[0].row);
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const int j = at.first + 16 * u;
-      if (j >= at.end) continue;
-      const int32_t page = ((uniform_ptr)of.row)[j >> shift];
-      at.page[u] = (int64_t)page < a.cache.pages ? page : -1;
-    }
+    for (int u = 0; u < 2; ++u) at.page[u] = row[min(at.first + 16 * u, end - 1) >> shift];
     return at;
   };
-  auto record = [&](const Place& at, int u) {
-    const bool here = at.page[u] >= 0;
-    return make_rsrc(cache + ((here ? at.page[u] : 0) * (int64_t)a.kv_heads + head) * (int64_t)(2 * part_bytes), here ? 2 * part_bytes : 0);
+  auto present = [&](const Place& at, int u) { return ((uint32_t)at.page[u] < (uint32_t)a.cache.pages) & (at.first + 16 * u < at.end); };
+  struct Source {                         // where a tile's halves are loaded from: their pages' record, and the first token there
+    __amdgpu_buffer_rsrc_t of[2];
+    int codes[2], scales[2];
   };
-  Half<D> x[2];
-  auto load_keys = [&](const Place& at) {
+  auto source = [&](const Place& at) {
+    Source from;
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      const __amdgpu_buffer_rsrc_t rsrc = record(at, u);
+      const bool here = present(at, u);
+      from.of[u] = make_rsrc(of_head + (uint32_t)(here ? at.page[u] : 0) * page_bytes, here ? 2 * part_bytes : 0);
       const int t0 = (at.first + 16 * u) & in_page;
-      load_words(rsrc, k_at, t0 * Kv4<D>::kCodes, x[u].k);
-      load_words(rsrc, scale_at, (Kv4<D>::kCodes << shift) + t0 * Kv4<D>::kScales, x[u].k_scale);
+      from.codes[u] = t0 * Kv4<D>::kCodes;
+      from.scales[u] = scales + t0 * Kv4<D>::kScales;
+    }
+    return from;
+  };
+  Half<D, F> x[2];
+  auto load_keys = [&](const Source& from) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      load_words(from.of[u], k_at, from.codes[u], x[u].k);
+      x[u].k_scale.load(from.of[u], scale_at, from.scales[u]);
     }
   };
-  auto load_value_scales = [&](const Place& at) {
+  auto load_value_scales = [&](const Source& from) {
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
-      load_words(record(at, u), scale_at, part_bytes + (Kv4<D>::kCodes << shift) + ((at.first + 16 * u) & in_page) * Kv4<D>::kScales, x[u].v_scale);
+    for (int u = 0; u < 2; ++u) x[u].v_scale.load(from.of[u], scale_at, part_bytes + from.scales[u]);
   };
-  auto load_values = [&](const Place& at) {
+  auto load_values = [&](const Source& from) {
 #pragma unroll
-    for (int u = 0; u < 2; ++u) load_words(record(at, u), v_at, part_bytes + ((at.first + 16 * u) & in_page) * Kv4<D>::kCodes, x[u].v);
-    load_value_scales(at);
+    for (int u = 0; u < 2; ++u) load_words(from.of[u], v_at, part_bytes + from.codes[u], x[u].v);
+    load_value_scales(from);
   };
   uint32_t saw[RT] = {};                  // whether a lane has seen a key
   bool all_saw = false;                   // a tile of which every row sees every key
-  Place at = place(wave), then = place(wave + kWaves);
+  Place at = {}, then = {};
   if (wave < tiles) {
-    load_keys(at);
-    load_values(at);
+    at = place(wave);
+    then = place(wave + kWaves);
+    const Source from = source(at);
+    load_keys(from);
+    __builtin_amdgcn_sched_barrier(0);    // in the loop's order, which its waits count by
+    load_values(from);
   }
 #pragma unroll 1
   for (int t = wave; t < tiles; t += kWaves) {
     const Place later = place(t + 2 * kWaves);
-    const bool whole = ((at.first >= at.begin) & (at.first + kTileKeys - 1 <= min(wave_first, at.end - 1)) & ((at.page[0] | at.page[1]) >= 0)) != 0;
+    const Source from = source(then);
+    const bool whole = ((at.first >= at.begin) & (at.first + kTileKeys - 1 <= min(wave_first, at.end - 1)) & present(at, 0) & present(at, 1)) != 0;
     all_saw |= whole;
     f32x4 s[RT][2];
     r.score(x, s);
@@ -362,75 +503,79 @@ __device__ __forceinline__ void walk_rows(const Decode<T>& a, const uint8_t* cac
 #pragma unroll
       for (int u = 0; u < 2; ++u) asm volatile("" : "+v"(s[rt][u]));
     __builtin_amdgcn_sched_barrier(0);
-    load_keys(then);
+    load_keys(from);
     __builtin_amdgcn_sched_barrier(0);
-    uint32_t seen[RT] = {};               // bit 4 u + i: whether a lane sees key i of its four of half u
+    uint32_t seen[RT][2] = {};            // bit i: whether a lane sees key i of its four of half u
     if (!whole) {
       asm volatile("");                   // a branch, not selects in every tile
 #pragma unroll
-      for (int rt = 0; rt < RT; ++rt)
+      for (int rt = 0; rt < RT; ++rt) {
 #pragma unroll
         for (int u = 0; u < 2; ++u)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const int j = at.first + 16 * u + 4 * h + i;
-            const bool sees = at.page[u] >= 0 && j >= at.begin && j <= min(last[rt], at.end - 1);
+            const bool sees = present(at, u) && j >= at.begin && j <= min(last[rt], at.end - 1);
             s[rt][u][i] = sees ? s[rt][u][i] : -INFINITY;
-            seen[rt] |= sees ? 1u << (4 * u + i) : 0u;
+            seen[rt][u] |= sees ? 1u << i : 0u;
           }
+        saw[rt] |= seen[rt][0] | seen[rt][1];
+      }
     }
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-      if (!whole) {                       // the scales of keys that tile rt's rows do not see
-        if (rt > 0) load_value_scales(at);
-        saw[rt] |= seen[rt];
+      // the scales of keys that tile rt's rows do not see are zero
+      if constexpr (F == 1) {
+        if (!whole) {
+          if (rt > 0) load_value_scales(source(at));
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
+          for (int u = 0; u < 2; ++u) x[u].v_scale.all.keep(seen[rt][u]);
+        }
+        r.add(rt, x, {x[0].v_scale.all, x[1].v_scale.all}, s[rt], scale);
+      } else {
+        Spread<D, F> by[2] = {x[0].v_scale.spread(), x[1].v_scale.spread()};
+        if (!whole) {
 #pragma unroll
-          for (int n = 0; n < kGroups / 2; ++n) {           // 8 / kGroups keys each
-            u32x4 keep;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) keep[i] = 0u - (seen[rt] >> (4 * u + (8 * n + 2 * i) / kGroups) & 1u);
-            x[u].v_scale[n] &= keep;
-          }
+          for (int u = 0; u < 2; ++u) by[u].keep(seen[rt][u]);
+        }
+        r.add(rt, x, by, s[rt], scale);
       }
-      r.add(rt, x, s[rt], scale);
     }
     __builtin_amdgcn_sched_barrier(0);
-    load_values(then);
+    load_values(from);
     at = then;
     then = later;
   }
 
   // The wavefronts' results, through LDS: all on the largest reference, then summed.
-  constexpr int kPitch = D + 4;
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
+    const int n = rt * S::kRows + col % S::kRows;
     const bool saw_one = all_saw || max_of_row((float)saw[rt]) != 0.0f;
     const float l = saw_one ? sum_of_row(r.l[rt]) : __uint_as_float(kSawNone);
-    if (h == 0) ml[wave][rt * kRows + col] = float2{r.m[rt], l};
+    if (h == 0 && col < S::kRows) lds.ml[wave][n] = float2{r.m[rt], l};
 #pragma unroll
     for (int t = 0; t < 2 * kGroups; ++t)
-      *reinterpret_cast<f32x4*>(lds + (wave * RT * kRows + rt * kRows + col) * kPitch + 16 * t + 4 * h) = r.o[rt][t];
+      if (F == 1 || col / S::kRows == t / 2 / S::kSets) *reinterpret_cast<f32x4*>(&lds.o[wave][n][16 * t + 4 * h]) = r.o[rt][t];
   }
   __syncthreads();
   constexpr int kChunks = D / 4;
 #pragma unroll
-  for (int c = threadIdx.x; c < RT * kRows * kChunks; c += kThreads) {
+  for (int c = threadIdx.x; c < kRows * kChunks; c += kThreads) {
     const int n = c / kChunks, d = 4 * (c % kChunks);
     if (index0 + n >= rows) continue;
     float m = -FLT_MAX, l = __uint_as_float(kSawNone);
 #pragma unroll
     for (int w = 0; w < kWaves; ++w)
-      if (__float_as_uint(ml[w][n].y) != kSawNone) m = fmaxf(m, ml[w][n].x);
+      if (__float_as_uint(lds.ml[w][n].y) != kSawNone) m = fmaxf(m, lds.ml[w][n].x);
     f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) {
-      const float2 of = ml[w][n];
+      const float2 of = lds.ml[w][n];
       if (__float_as_uint(of.y) == kSawNone) continue;
       const float by = __builtin_amdgcn_exp2f(of.x - m);
       l = __builtin_fmaf(by, of.y, l);
-      const f32x4 add = *reinterpret_cast<const f32x4*>(lds + (w * RT * kRows + n) * kPitch + d);
+      const f32x4 add = *reinterpret_cast<const f32x4*>(&lds.o[w][n][d]);
 #pragma unroll
       for (int i = 0; i < 4; ++i) o[i] = __builtin_fmaf(by, add[i], o[i]);
     }
@@ -438,61 +583,71 @@ __device__ __forceinline__ void walk_rows(const Decode<T>& a, const uint8_t* cac
   }
 }
 
-template <typename T, int D, int RT>
-__global__ __launch_bounds__(kThreads, sizeof(T) == 2 && RT == 1 ? 3 : 2) void decode_kv4_kernel(const Decode<T> a, const uint8_t* cache, const Kv4Plan p, const Parts parts, int prefix_groups, bool sorted) {
-  __shared__ __align__(16) float lds[kWaves * RT * kRows * (D + 4)];
-  __shared__ float2 ml[kWaves][RT * kRows];
+// SHARE: some workgroups take the prefix for all requests.
+template <typename T, int D, int RT, int F, bool SHARE>
+__global__ __launch_bounds__(kThreads, SHARE || RT > 1 ? 2 : F > 1 ? 4 : 3) void decode_kv4_kernel(const Decode<T> a, const uint8_t* cache, const Kv4Plan p, const Parts parts, int prefix_groups, bool sorted) {
+  constexpr int kOwnRows = RT * 16 / F;
+  __shared__ union {
+    Shared<D, kOwnRows> own;
+    Shared<D, SHARE ? kWideRows : kOwnRows> wide;
+  } lds;
   const int prefix = (int)min(a.prefix, min(a.max_len, a.table_stride << a.cache.page_shift));
   // the heads in turn; of the rest, work on the prefix (long) before the requests' own keys
   const int head = (int)blockIdx.x % a.kv_heads, turn = (int)blockIdx.x / a.kv_heads;
   KeyRange range[2] = {{a.table, 0, 0}, {a.table, 0, 0}};
-  int request = -1, index0, part;
-  if (turn < prefix_groups) {
-    index0 = turn % p.prefix_tiles * (RT * kRows);
-    part = turn / p.prefix_tiles;
-    const int per = ((prefix + p.prefix_parts - 1) / p.prefix_parts + kStepKeys - 1) / kStepKeys * kStepKeys;
-    range[0].begin = min(part * per, prefix);
-    range[0].end = min(range[0].begin + per, prefix);
-  } else {
-    int i = turn - prefix_groups;
-    part = i % p.own_parts;
-    i /= p.own_parts;
-    index0 = i % p.own_tiles * (RT * kRows);
-    request = i / p.own_tiles;
-    if (sorted) request = longest_first(a, request);
-    const int len = request_len(a, request), from = min(p.share ? prefix : 0, len), base = from & ~(kTileKeys - 1);
-    const int per = ((len - base + p.own_parts - 1) / p.own_parts + kStepKeys - 1) / kStepKeys * kStepKeys;
-    const int lo = max(min(base + part * per, len), from), hi = min(base + (part + 1) * per, len);
-    range[0].begin = lo;
-    range[0].end = min(hi, prefix);
-    range[1] = {a.table + request * a.table_stride, max(lo, prefix), hi};
-    if (p.share) part += p.prefix_parts;
+  if constexpr (SHARE) {
+    if (turn < prefix_groups) {
+      const int index0 = turn % p.prefix_tiles * kWideRows, part = turn / p.prefix_tiles;
+      const int per = ((prefix + p.prefix_parts - 1) / p.prefix_parts + kStepKeys - 1) / kStepKeys * kStepKeys;
+      range[0].begin = min(part * per, prefix);
+      range[0].end = min(range[0].begin + per, prefix);
+      return walk_rows<T, D, kWideRows / 16, 1>(a, cache, p, parts, head, -1, index0, range, part, lds.wide);
+    }
   }
-  walk_rows<T, D, RT>(a, cache, p, parts, head, request, index0, range, part, lds, ml);
+  int i = turn - prefix_groups, part = i % p.own_parts;
+  i /= p.own_parts;
+  const int index0 = i % p.own_tiles * kOwnRows;
+  int request = i / p.own_tiles;
+  if (sorted) request = longest_first(a, request);
+  const int len = request_len(a, request), from = min(SHARE ? prefix : 0, len), base = from & ~(kTileKeys - 1);
+  const int per = ((len - base + p.own_parts - 1) / p.own_parts + kStepKeys - 1) / kStepKeys * kStepKeys;
+  const int lo = max(min(base + part * per, len), from), hi = min(base + (part + 1) * per, len);
+  range[0].begin = lo;
+  range[0].end = min(hi, prefix);
+  range[1] = {a.table + request * a.table_stride, max(lo, prefix), hi};
+  if (SHARE) part += p.prefix_parts;
+  walk_rows<T, D, RT, F>(a, cache, p, parts, head, request, index0, range, part, lds.own);
 }
 
-template <typename T, int D, int RT>
+template <typename T, int D, int RT, int F>
 hipError_t launch_kv4(const Decode<T>& a, const uint8_t* cache, const Kv4Plan& p, const Parts& parts, hipStream_t stream) {
   const int64_t prefix_groups = p.prefix_groups(), own_groups = a.requests * p.own_tiles * p.own_parts;
-  decode_kv4_kernel<T, D, RT><<<dim3((unsigned)((prefix_groups + own_groups) * a.kv_heads)), kThreads, 0, stream>>>(a, cache, p, parts, (int)prefix_groups, false);
+  const dim3 grid((unsigned)((prefix_groups + own_groups) * a.kv_heads));
+  if (p.share) decode_kv4_kernel<T, D, RT, F, true><<<grid, kThreads, 0, stream>>>(a, cache, p, parts, (int)prefix_groups, false);
+  else decode_kv4_kernel<T, D, RT, F, false><<<grid, kThreads, 0, stream>>>(a, cache, p, parts, 0, false);
   if (p.parts() > 1) launch_join<T, D>(a, p.line_rows, p.parts(), parts, stream);
   return hipGetLastError();
 }
 
 template <typename T, int D>
 hipError_t launch_kv4_dim(const Decode<T>& a, const uint8_t* cache, void* workspace, size_t workspace_bytes, hipStream_t stream) {
-  Kv4Plan p = make_kv4_plan(a.requests, a.fresh, a.q_heads, a.kv_heads, a.max_len, a.prefix, true);
+  Kv4Plan p = make_kv4_plan(a.requests, a.fresh, a.q_heads, a.kv_heads, D, a.max_len, a.prefix, true);
   const size_t need = parts_bytes(p.parts(), p.line_rows, D);
-  if (need > 0 && (workspace == nullptr || workspace_bytes < need)) p = make_kv4_plan(a.requests, a.fresh, a.q_heads, a.kv_heads, a.max_len, a.prefix, false);
+  if (need > 0 && (workspace == nullptr || workspace_bytes < need)) p = make_kv4_plan(a.requests, a.fresh, a.q_heads, a.kv_heads, D, a.max_len, a.prefix, false);
   const Parts parts = p.parts() > 1 ? place_parts<D>(workspace, p.parts(), p.line_rows) : Parts{nullptr, nullptr};
-  return launch_kv4<T, D, 1>(a, cache, p, parts, stream);
+  switch (p.own_rows) {
+    case 4: if constexpr (D == 128) return launch_kv4<T, D, 1, 4>(a, cache, p, parts, stream);
+    case 8: return launch_kv4<T, D, 1, 2>(a, cache, p, parts, stream);
+    case 16: return launch_kv4<T, D, 1, 1>(a, cache, p, parts, stream);
+    default: return launch_kv4<T, D, 2, 1>(a, cache, p, parts, stream);
+  }
 }
 
 }  // namespace
 }  // namespace attention
 
 size_t attention_decode_kv4_workspace_bytes(int64_t requests, int fresh, int q_heads, int kv_heads, int head_dim, int64_t max_len, int64_t prefix) {
-  const attention::Kv4Plan p = attention::make_kv4_plan(requests, fresh, q_heads, kv_heads, max_len, prefix, true);
+  const attention::Kv4Plan p = attention::make_kv4_plan(requests, fresh, q_heads, kv_heads, head_dim, max_len, prefix, true);
   return attention::parts_bytes(p.parts(), p.line_rows, head_dim);
 }
 

@@ -15,7 +15,7 @@
  *   M = max|w|;  s = -M / 8 if max w > -min w, else M / 8   (binary32; +0 if M = 0)
  *   c = clip(rne(fl32(w / s)), -8, 7), 0 if M = 0;  held value = c * binary16(s).
  * A group that holds an infinity or a NaN, or whose s binary16 does not reach (M >= 524160), has the
- * scale NaN: all of it reads as NaN.
+ * codes c = 0 and the scale NaN: all of it reads as NaN.
  *   cache  uint8 [pages, kv_heads, 2, page_size * (D/2 + D/16)], D = head_dim: for each page
  *          and head the keys, then the values, each page_size tokens' codes (D/2 bytes a
  *          token) and behind them their scales [page_size, D/32].  With u = c + 8, G = D/32:
@@ -42,7 +42,7 @@ extern "C" {
  *
  *   k, v            device, bf16 [tokens, kv_heads, head_dim] (keys as ssq_qk_norm_rope
  *                   rotates them)
- *   tokens          >= 0; tokens * kv_heads * head_dim < 2^35
+ *   tokens          >= 0; ceil(tokens * head_dim / 2048) * kv_heads < 2^24
  *   slots           device, int32 [tokens]: page * page_size + offset; a slot outside
  *                   [0, pages * page_size) is not stored.  Two tokens of a call must not have
  *                   the same slot (what it then holds is a mixture of both).  Bytes of other

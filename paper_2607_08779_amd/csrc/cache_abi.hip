@@ -26,7 +26,8 @@ int kv4_store(const T* k, int64_t k_stride, const T* v, int64_t v_stride, int64_
   if (tokens < 0 || tokens > kMaxLen || !valid_heads(kv_heads, kv_heads) || !valid_dim(head_dim) || !valid_page(page_size) || pages < 0 ||
       pages > INT32_MAX / page_size)
     return SSQ_EINVAL;
-  if (tokens * kv_heads * (head_dim / 8) >= 256 * ssq::kMaxGroups) return SSQ_EINVAL;       // a thread for 8 elements
+  const int64_t together = 256 / (head_dim / 8);            // tokens of a head that a workgroup takes
+  if ((tokens + together - 1) / together * kv_heads >= ssq::kMaxGroups) return SSQ_EINVAL;
   if (!valid_stride<T>(k_stride, kv_heads, head_dim) || !valid_stride<T>(v_stride, kv_heads, head_dim) ||
       (k_held != nullptr && !valid_stride<T>(k_held_stride, kv_heads, head_dim)) || (v_held != nullptr && !valid_stride<T>(v_held_stride, kv_heads, head_dim)))
     return SSQ_EINVAL;

@@ -66,7 +66,8 @@ def on_grid(x):
     scale = s.half().squeeze(-1)
     bad = ~torch.isfinite(w).all(-1) | ~torch.isfinite(scale)
     scale = torch.where(bad, torch.tensor(float("nan"), dtype=torch.float16), scale)
-    return torch.nan_to_num(c + 8).to(torch.int32).flatten(-2), scale
+    c = torch.where(bad[..., None], torch.zeros(()), c)
+    return (c + 8).to(torch.int32).flatten(-2), scale
 
 
 def attend(q, k, v, k_size, v_size, last, scale):

@@ -35,7 +35,7 @@ STORE = dict(k=at(0), k_stride=128, v=at(1), v_stride=128, tokens=4, kv_heads=2,
     dict(tokens=-1), dict(tokens=(1 << 30) + 1), dict(kv_heads=0), dict(kv_heads=1 << 17), dict(head_dim=32), dict(head_dim=96), dict(head_dim=256), dict(page_size=8),
     dict(page_size=48), dict(page_size=2048), dict(pages=-1), dict(pages=1 << 27), dict(k_stride=127), dict(k_stride=64), dict(v_stride=132), dict(k_stride=1 << 25),
     dict(k_held_stride=120), dict(v_held_stride=0), dict(k=None), dict(v=None), dict(slots=None), dict(cache=None), dict(k_held=at(0), k_held_stride=256),
-    dict(v_held=at(1), v_held_stride=256), dict(tokens=1 << 28, kv_heads=2),
+    dict(v_held=at(1), v_held_stride=256), dict(tokens=1 << 29, kv_heads=2),
 ])
 def test_store_refuses(given):
     for name in ("ssq_kv4_store", "ssq_kv4_store_f32"):
@@ -52,10 +52,12 @@ def test_store_refuses_misaligned(which, n):
 
 
 def test_store_refuses_what_no_launch_holds():
-    """A thread for 8 elements, fewer than 2^32 of them."""
+    """A workgroup for 16 tokens of a head of 128, 32 of a head of 64, fewer than 2^24 of them."""
     given = dict(kv_heads=16, head_dim=128, k_stride=2048, v_stride=2048, k_held=None, v_held=None, k=off(8))
-    assert call("ssq_kv4_store", STORE, {**given, "tokens": 1 << 24}) == EINVAL
-    assert call("ssq_kv4_store", STORE, {**given, "tokens": (1 << 24) - 1}) == EALIGN
+    assert call("ssq_kv4_store", STORE, {**given, "tokens": (1 << 24) - 15}) == EINVAL
+    assert call("ssq_kv4_store", STORE, {**given, "tokens": (1 << 24) - 16}) == EALIGN
+    assert call("ssq_kv4_store", STORE, {**given, "head_dim": 64, "tokens": (1 << 25) - 31}) == EINVAL
+    assert call("ssq_kv4_store", STORE, {**given, "head_dim": 64, "tokens": (1 << 25) - 32}) == EALIGN
 
 
 DECODE = dict(q=at(0), q_stride=512, requests=2, fresh=1, q_heads=8, kv_heads=2, head_dim=64, scale=0.125, cache=at(1), pages=5, page_size=16, table=at(2),

@@ -8,6 +8,7 @@ It fails loudly if the library has not been built: there is no fallback.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from typing import Optional, Tuple
 
@@ -589,16 +590,20 @@ _EXPORTS["ssq_page_collect_workspace_size"] = (ctypes.c_size_t, [_L, _I])
 _EXPORTS["ssq_page_copy"] = (_I, [_P, _I, _L, _L, _P, _P, _L, _P])
 
 
-def _launch(fn, name: str, device: torch.device, tensors, *args) -> None:
-    """fn(*args, stream) on the current stream of `device`, where all of `tensors` (or None) have to be."""
-    for t in tensors:
-        if t is not None and t.device != device:
-            raise ValueError(f"all tensors must be on one device (got {device} and {t.device})")
-    if device.index == torch.cuda.current_device():
-        st = fn(*args, _stream(device))
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
+def _launch(fn, name: str, first: torch.Tensor, others, *args) -> None:
+    """fn(*args, stream) on the current stream of the device of ``first``, where all ``others`` (or None) have to be."""
+    index = first.get_device()
+    for t in others:
+        if t is not None and t.get_device() != index:
+            raise ValueError(f"all tensors must be on one device (got {first.device} and {t.device})")
+    if index == _current_device():
+        st = fn(*args, _stream(first.device))
     else:
-        with torch.cuda.device(device):
-            st = fn(*args, _stream(device))
+        with torch.cuda.device(index):
+            st = fn(*args, _stream(first.device))
     if st:
         _check(name, st)
 
@@ -632,12 +637,14 @@ def ssq_kv4_store(k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, cache: 
     khp = vhp = None
     if held is True:
         held = torch.empty_like(k, memory_format=_PACKED), torch.empty_like(v, memory_format=_PACKED)
-    if held:
+        khs = vhs = hk * dim
+        khp, vhp = held[0].data_ptr(), held[1].data_ptr()
+    elif held:
         if held[0].shape != k.shape or held[1].shape != v.shape:
             raise ValueError("held must be tensors like k and v")
         khs, vhs = _heads(held[0], "held k", dtype), _heads(held[1], "held v", dtype)
         khp, vhp = _ptr(held[0]), _ptr(held[1])
-    _launch(fn, name, k.device, (v, slots, cache, *(held or ())), _ptr(k), ks, _ptr(v), vs, tokens, hk, dim,
+    _launch(fn, name, k, (v, slots, cache, *(held or ())), _ptr(k), ks, _ptr(v), vs, tokens, hk, dim,
             _flat(slots, "slots", torch.int32, (tokens,)), cp, pages, page_size, khp, khs, vhp, vhs)
     return held or None
 
@@ -672,7 +679,7 @@ def ssq_attention_decode_kv4(q: torch.Tensor, cache: torch.Tensor, table: torch.
             workspace = torch.empty(size, dtype=torch.uint8, device=q.device)
     elif not workspace.is_contiguous():
         raise ValueError("workspace must be contiguous")
-    _launch(fn, name, q.device, (cache, table, lens, out, workspace), _ptr(q), stride, n, fresh, hq, hk, dim,
+    _launch(fn, name, q, (cache, table, lens, out, workspace), _ptr(q), stride, n, fresh, hq, hk, dim,
             dim ** -0.5 if scale is None else scale, cp, pages, page_size, _flat(table, "table", torch.int32, (n, width)), width,
             _flat(lens, "lens", torch.int32, (n,)), max_len, prefix, _ptr(out), hq * dim, _ptr(workspace),
             0 if workspace is None else workspace.numel() * workspace.element_size())
@@ -709,25 +716,52 @@ def ssq_page_fork(parents: torch.Tensor, lens: torch.Tensor, table: torch.Tensor
         to = (_flat(table_out, "table out", i32, (n, width)), _flat(lens_out, "lens out", i32, (n,)), _flat(src, "src", i32, (n,)),
               _flat(dst, "dst", i32, (n,)), _flat(after, "taken after", i32, (1,)))
     fn, name = _entry("ssq_page_fork", torch.bfloat16)
-    _launch(fn, name, dev, (lens, table, free_pages, taken, table_out, lens_out, src, dst, after), _flat(parents, "parents", i32, (n,)), n,
+    _launch(fn, name, parents, (lens, table, free_pages, taken, table_out, lens_out, src, dst, after), _flat(parents, "parents", i32, (n,)), n,
             _flat(lens, "lens", i32, (rows,)), _flat(table, "table", i32, (rows, stride)), rows, stride,
             _flat(free_pages, "free_pages", i32, free_pages.shape[:1]), free_pages.numel(),
             None if taken is None else _flat(taken, "taken", i32, (1,)), page_size, to[0], width, *to[1:])
     return table_out, lens_out, src, dst, after
 
 
-def _pool_arguments(lens, table, pages, pinned, compact, workspace):
+@functools.lru_cache(maxsize=64)
+def _collect_bytes(pages: int, compact: bool) -> int:
+    return int(lib().ssq_page_collect_workspace_size(pages, int(compact)))
+
+
+def _collect(name: str, lens, table, page_size, pages, pinned, sizes, out, workspace, compact: bool):
+    """ssq_page_collect or ssq_page_compact into int32 arrays of `sizes`, allocated with the workspace where they are not given."""
     if lens.dim() != 1 or table.dim() != 2:
         raise ValueError("lens must be [requests] and table [requests, pages]")
     if pages < 0:
         raise ValueError("pages must not be negative")
     n, width = table.shape
-    if workspace is None:
-        workspace = torch.empty(lib().ssq_page_collect_workspace_size(pages, compact), dtype=torch.uint8, device=lens.device)
-    elif not workspace.is_contiguous():
+    i32, need = torch.int32, _collect_bytes(pages, compact)
+    if workspace is not None and not workspace.is_contiguous():
         raise ValueError("workspace must be contiguous")
-    return (_flat(lens, "lens", torch.int32, (n,)), n, _flat(table, "table", torch.int32, (n, width)), width,
-            None if pinned is None else _flat(pinned, "pinned", torch.uint8, (pages,)), workspace)
+    if out is None:
+        total = sum(sizes)
+        scratch = 0 if workspace is not None else -total % 64 + (need + 3) // 4
+        buf = torch.empty(total + scratch, dtype=i32, device=lens.device)
+        base = _ptr(buf)
+        out = torch.split_with_sizes(buf, (*sizes, scratch))[:-1]
+        to, at = [], base
+        for size in sizes:
+            to.append(at)
+            at += 4 * size
+        if compact:
+            out = (out[0].view(n, width), *out[1:])
+        if workspace is None:                   # behind the outputs, from the next 256 bytes on
+            scratch_at, scratch_bytes = base + 4 * (total + -total % 64), need
+    else:
+        to = [_flat(x, "an output", i32, (n, width) if compact and i == 0 else (size,)) for i, (x, size) in enumerate(zip(out, sizes))]
+        if workspace is None:
+            workspace = torch.empty(need, dtype=torch.uint8, device=lens.device)
+    if workspace is not None:
+        scratch_at, scratch_bytes = _ptr(workspace), workspace.numel() * workspace.element_size()
+    fn, name = _entry(name, torch.bfloat16)
+    _launch(fn, name, lens, (table, pinned, *out, workspace), _flat(lens, "lens", i32, (n,)), n, _flat(table, "table", i32, (n, width)), width, page_size,
+            pages, None if pinned is None else _flat(pinned, "pinned", torch.uint8, (pages,)), *to, scratch_at, scratch_bytes)
+    return out
 
 
 def ssq_page_collect(lens: torch.Tensor, table: torch.Tensor, page_size: int, pages: int, pinned: Optional[torch.Tensor] = None,
@@ -735,21 +769,9 @@ def ssq_page_collect(lens: torch.Tensor, table: torch.Tensor, page_size: int, pa
     """The pages of a pool of ``pages`` that no request holds, on the current stream: request r holds the
     first ceil(lens[r] / page_size) entries of ``table[r]`` (int32 [requests, pages]); ``pinned`` (uint8 [pages])
     is not 0 for pages that are held in any case.  Returns (free_pages [pages], ascending, then -1; count [1]), int32.
-    ``out`` reuses buffers; ``workspace`` (uint8, any contents, ``ssq_page_collect_workspace_size`` bytes)
+    ``out`` = these two reuses buffers; ``workspace`` (uint8, any contents, ``ssq_page_collect_workspace_size`` bytes)
     is allocated where it is not given."""
-    lp, n, tp, width, pp, workspace = _pool_arguments(lens, table, pages, pinned, 0, workspace)
-    i32 = torch.int32
-    if out is None:
-        buf = torch.empty(pages + 1, dtype=i32, device=lens.device)
-        free, count = torch.split_with_sizes(buf, (pages, 1))
-        to = _ptr(buf), _ptr(buf) + 4 * pages
-    else:
-        free, count = out
-        to = _flat(free, "free pages", i32, (pages,)), _flat(count, "count", i32, (1,))
-    fn, name = _entry("ssq_page_collect", torch.bfloat16)
-    _launch(fn, name, lens.device, (table, pinned, free, count, workspace), lp, n, tp, width, page_size, pages, pp, *to, _ptr(workspace),
-            workspace.numel() * workspace.element_size())
-    return free, count
+    return _collect("ssq_page_collect", lens, table, page_size, pages, pinned, (pages, 1), out, workspace, False)
 
 
 def ssq_page_compact(lens: torch.Tensor, table: torch.Tensor, page_size: int, pages: int, pinned: Optional[torch.Tensor] = None,
@@ -758,28 +780,12 @@ def ssq_page_compact(lens: torch.Tensor, table: torch.Tensor, page_size: int, pa
     numbers, free_pages [pages] and count [1] after the moves, src, dst [pages // 2]: the moves, then -1, moved [1]), int32.
     The moves are to be made in every layer (``ssq_page_copy``) before its cache is next used.  ``out`` = these
     six reuses buffers; its table may be ``table`` itself."""
-    lp, n, tp, width, pp, workspace = _pool_arguments(lens, table, pages, pinned, 1, workspace)
-    i32, half = torch.int32, pages // 2
-    if out is None:
-        sizes = (n * width, pages, 1, half, half, 1)
-        buf = torch.empty(sum(sizes), dtype=i32, device=lens.device)
-        table_out, free, count, src, dst, moved = torch.split_with_sizes(buf, sizes)
-        table_out = table_out.view(n, width)
-        base = _ptr(buf)
-        to = [base + 4 * sum(sizes[:i]) for i in range(6)]
-    else:
-        table_out, free, count, src, dst, moved = out
-        to = (_flat(table_out, "table out", i32, (n, width)), _flat(free, "free pages", i32, (pages,)), _flat(count, "count", i32, (1,)),
-              _flat(src, "src", i32, (half,)), _flat(dst, "dst", i32, (half,)), _flat(moved, "moved", i32, (1,)))
-    fn, name = _entry("ssq_page_compact", torch.bfloat16)
-    _launch(fn, name, lens.device, (table, pinned, table_out, free, count, src, dst, moved, workspace), lp, n, tp, width, page_size, pages, pp,
-            *to, _ptr(workspace), workspace.numel() * workspace.element_size())
-    return table_out, free, count, src, dst, moved
+    return _collect("ssq_page_compact", lens, table, page_size, pages, pinned, (table.numel(), pages, 1, pages // 2, pages // 2, 1), out, workspace, True)
 
 
 def ssq_page_collect_workspace_size(pages: int, compact: bool = False) -> int:
     """Bytes of scratch for ssq_page_collect, or (``compact``) for ssq_page_compact."""
-    return int(lib().ssq_page_collect_workspace_size(pages, int(compact)))
+    return _collect_bytes(pages, bool(compact))
 
 
 def ssq_page_copy(caches, src: torch.Tensor, dst: torch.Tensor) -> None:
@@ -789,13 +795,14 @@ def ssq_page_copy(caches, src: torch.Tensor, dst: torch.Tensor) -> None:
     caches = list(caches)
     if not caches:
         return
-    shape, size, dev = caches[0].shape, caches[0].element_size(), caches[0].device
+    shape, dtype, size = caches[0].shape, caches[0].dtype, caches[0].element_size()
     if not shape or src.dim() != 1:
         raise ValueError("caches must be [pages, ...], src and dst [entries]")
     pages, page_bytes = shape[0], shape[1:].numel() * size
     for c in caches:
-        if c.dim() == 0 or c.shape[0] != pages or c.shape[1:].numel() * c.element_size() != page_bytes or not c.is_contiguous() or c.device != dev:
+        alike = c.shape == shape and c.dtype == dtype or c.dim() > 0 and c.shape[0] == pages and c.shape[1:].numel() * c.element_size() == page_bytes
+        if not alike or not c.is_contiguous():
             raise ValueError("caches must be contiguous, on one device, and have the same pages and bytes a page")
     fn, name = _entry("ssq_page_copy", torch.bfloat16)
-    _launch(fn, name, dev, (src, dst), (ctypes.c_void_p * len(caches))(*(_ptr(c) for c in caches)), len(caches), page_bytes, pages,
+    _launch(fn, name, caches[0], (*caches[1:], src, dst), (ctypes.c_void_p * len(caches))(*(_ptr(c) for c in caches)), len(caches), page_bytes, pages,
             _flat(src, "src", torch.int32, src.shape), _flat(dst, "dst", torch.int32, src.shape), src.shape[0])

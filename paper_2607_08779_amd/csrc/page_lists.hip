@@ -324,7 +324,7 @@ __global__ __launch_bounds__(kThreads) void rename_kernel(const PageCollect a, c
 constexpr int kOneThreads = 1024, kOneWaves = kOneThreads / 64;
 constexpr int kOnePages = 1 << 17, kOneWords = kOnePages / 32, kOneRows = 2048;
 constexpr int64_t kOneEntries = 1 << 14;          // of a table that every workgroup marks for itself
-constexpr int kOnePerGroup = 2048;                // pages of a workgroup's share
+constexpr int kOneShare = 512, kOneGroups = 256;  // pages of a workgroup, where so many workgroups suffice
 constexpr int kOneAhead = 16;                     // table entries that a lane has under way
 
 struct OneLds {
@@ -367,7 +367,7 @@ __device__ __forceinline__ uint32_t before_in_one(uint32_t v, uint32_t (&waves)[
 }
 
 template <bool COMPACT, bool MARKED>
-__global__ __launch_bounds__(kOneThreads) void pool_kernel(const PageCollect a, const uint8_t* marks) {
+__global__ __launch_bounds__(kOneThreads) void pool_kernel(const PageCollect a, const uint8_t* marks, int share) {
   __shared__ OneLds lds;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int pages = (int)a.pages, words = (pages + 31) / 32, rows = (int)a.requests, stride = (int)a.stride;
@@ -376,13 +376,22 @@ __global__ __launch_bounds__(kOneThreads) void pool_kernel(const PageCollect a, 
   if constexpr (MARKED) {
     // 16 marks of a byte each to two bits; what lies behind the pages is marked as held
     auto four = [](uint32_t x) { return ((x & 0x01010101u) * 0x10204080u) >> 28; };
-    for (int i = tid; i < 2 * words; i += kOneThreads) {
-      const u32x4 m = *reinterpret_cast<const u32x4*>(marks + 16 * i);
-      uint32_t held = 0, pinned = 0;
+    constexpr int kLoads = 8;
+    for (int i0 = tid; i0 < 2 * words; i0 += kOneThreads * kLoads) {
+      u32x4 m[kLoads];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) held |= four(m[j]) << (4 * j), pinned |= four(m[j] >> 1) << (4 * j);
-      reinterpret_cast<uint16_t*>(lds.held)[i] = (uint16_t)held;
-      reinterpret_cast<uint16_t*>(lds.pinned)[i] = (uint16_t)pinned;
+      for (int k = 0; k < kLoads; ++k) m[k] = *reinterpret_cast<const u32x4*>(marks + 16 * min(i0 + kOneThreads * k, 2 * words - 1));
+#pragma unroll
+      for (int k = 0; k < kLoads; ++k) {
+        const int i = i0 + kOneThreads * k;
+        uint32_t held = 0, pinned = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) held |= four(m[k][j]) << (4 * j), pinned |= four(m[k][j] >> 1) << (4 * j);
+        if (i < 2 * words) {
+          reinterpret_cast<uint16_t*>(lds.held)[i] = (uint16_t)held;
+          reinterpret_cast<uint16_t*>(lds.pinned)[i] = (uint16_t)pinned;
+        }
+      }
     }
     __syncthreads();
   } else {
@@ -452,7 +461,8 @@ __global__ __launch_bounds__(kOneThreads) void pool_kernel(const PageCollect a, 
   const uint32_t holes = COMPACT ? free_to(used) : 0, pinned_below = COMPACT ? pinned_to(used) : 0, moves = holes - (pinned_all - pinned_below);
 
   // This workgroup's pages.
-  for (int i = (int)blockIdx.x * kOnePerGroup + tid; i < min(pages, ((int)blockIdx.x + 1) * kOnePerGroup); i += kOneThreads) {
+  const int end = min(pages, ((int)blockIdx.x + 1) * share);
+  for (int i = (int)blockIdx.x * share + tid; i < end; i += kOneThreads) {
     const bool held = lds.held[i / 32] >> (i % 32) & 1u;
     const uint32_t at = free_to(i);
     if (!COMPACT) {
@@ -468,7 +478,7 @@ __global__ __launch_bounds__(kOneThreads) void pool_kernel(const PageCollect a, 
     }
   }
   // The entries behind the lists.
-  for (int i = (int)blockIdx.x * kOnePerGroup + tid; i < min(pages, ((int)blockIdx.x + 1) * kOnePerGroup); i += kOneThreads) {
+  for (int i = (int)blockIdx.x * share + tid; i < end; i += kOneThreads) {
     if (i >= (int)free_all) a.free_pages[i] = -1;
     if (COMPACT && i < pages / 2 && i >= (int)moves) a.src[i] = a.dst[i] = -1;
   }
@@ -567,19 +577,20 @@ hipError_t launch_page_collect(const PageCollect& a, bool compact, void* workspa
   const dim3 blocks((unsigned)s.blocks);
   const int64_t row_groups = (a.stride + 4 * kThreads - 1) / (4 * kThreads);
   const dim3 rows((unsigned)(a.requests * row_groups));
-  const dim3 groups((unsigned)max((a.pages + kOnePerGroup - 1) / kOnePerGroup, (int64_t)1));
+  const int share = (int)max((int64_t)kOneShare, (a.pages + kOneGroups - 1) / kOneGroups);
+  const dim3 groups((unsigned)max((a.pages + share - 1) / share, (int64_t)1));
   const bool few = a.pages <= kOnePages && a.requests <= kOneRows;
   // in place, rows would be renamed while other workgroups still mark
   if (few && a.requests * a.stride <= kOneEntries && !(compact && a.table_out == a.table && a.stride > 0)) {
-    if (compact) pool_kernel<true, false><<<groups, kOneThreads, 0, stream>>>(a, nullptr);
-    else pool_kernel<false, false><<<groups, kOneThreads, 0, stream>>>(a, nullptr);
+    if (compact) pool_kernel<true, false><<<groups, kOneThreads, 0, stream>>>(a, nullptr, share);
+    else pool_kernel<false, false><<<groups, kOneThreads, 0, stream>>>(a, nullptr, share);
     return hipGetLastError();
   }
   clear_kernel<<<blocks, kThreads, 0, stream>>>(a, s);
   if (rows.x > 0) mark_kernel<<<rows, kThreads, 0, stream>>>(a, s, row_groups);
   if (few) {
-    if (compact) pool_kernel<true, true><<<groups, kOneThreads, 0, stream>>>(a, s.marks);
-    else pool_kernel<false, true><<<groups, kOneThreads, 0, stream>>>(a, s.marks);
+    if (compact) pool_kernel<true, true><<<groups, kOneThreads, 0, stream>>>(a, s.marks, share);
+    else pool_kernel<false, true><<<groups, kOneThreads, 0, stream>>>(a, s.marks, share);
     return hipGetLastError();
   }
   count_kernel<<<blocks, kThreads, 0, stream>>>(a, s);

@@ -649,10 +649,15 @@ def ssq_kv4_store(k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, cache: 
     return held or None
 
 
+@functools.lru_cache(maxsize=256)
+def _decode_kv4_bytes(*sizes: int) -> int:
+    return int(lib().ssq_attention_decode_kv4_workspace_size(*sizes))
+
+
 def ssq_attention_decode_kv4_workspace_size(requests: int, fresh: int, q_heads: int, kv_heads: int, head_dim: int,
                                             max_len: int, prefix: int = 0) -> int:
     """Bytes of scratch that let ssq_attention_decode_kv4 split long caches and share a prefix."""
-    return int(lib().ssq_attention_decode_kv4_workspace_size(requests, fresh, q_heads, kv_heads, head_dim, max_len, prefix))
+    return _decode_kv4_bytes(requests, fresh, q_heads, kv_heads, head_dim, max_len, prefix)
 
 
 def ssq_attention_decode_kv4(q: torch.Tensor, cache: torch.Tensor, table: torch.Tensor, lens: torch.Tensor, max_len: int,
@@ -674,7 +679,7 @@ def ssq_attention_decode_kv4(q: torch.Tensor, cache: torch.Tensor, table: torch.
     elif out.shape != q.shape or out.dtype != dtype or not out.is_contiguous():
         raise ValueError("out must be a contiguous tensor like q")
     if workspace is None:
-        size = lib().ssq_attention_decode_kv4_workspace_size(n, fresh, hq, hk, dim, max_len, prefix)
+        size = _decode_kv4_bytes(n, fresh, hq, hk, dim, max_len, prefix)
         if size:
             workspace = torch.empty(size, dtype=torch.uint8, device=q.device)
     elif not workspace.is_contiguous():

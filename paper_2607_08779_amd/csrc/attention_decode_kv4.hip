@@ -19,6 +19,21 @@
 // when a tile's maximum of that row exceeds it by more than kSlack, a sum of -0 for rows that saw no
 // key.  Codes are finite whatever their bits, so that what is hidden can only enter through its
 // scales: they are set to zero, and the scores to -inf, in tiles that hold hidden keys.
+//
+// Workgroups are of two kinds: on a request's own keys, up to 8, 16 or 32 rows of it; on a shared
+// prefix, 32 rows of all requests.  Their four wavefronts take the keys 32 at a time, each for itself, and
+// meet in LDS at the end; parts of a row are joined by a second launch (attention_join.h).  The next keys
+// are loaded into the registers of these as soon as the scores are formed, the next values after
+// the product, so that three or four workgroups fit a CU (48 requests of 4096 to 8191 keys, 8 key/value
+// heads: 91 us with two sets of registers and two workgroups a CU, 71 so).
+//
+// Own keys are bound by memory: 96 requests of 8192 keys (908 MB) take 158 us, 5.75 TB/s; reading the
+// same bytes in the same order, without arithmetic, takes 148.  48 requests of 4096 to 8191 keys (337 MB):
+// 72 us, of which 4.7 are the joining launch and the rest ends unevenly.  One request of 16383 keys: 12.2,
+// of which 3.4 are the joining launch; the walk's 9 are a launch, four loads that wait for each other and
+// four tiles.  The prefix is bound by the vector unit: 16 rows and 32 keys take about 170
+// instructions, a third of which unpack (shared by two tiles of rows) and half of which apply scales,
+// beside 24 products: 64 requests of 1 to 1024 keys behind 8192 take 34.5 us (50 MB, 9.2 GFLOP).
 #include "attention_join.h"
 #include "kv4.h"
 
@@ -33,7 +48,7 @@ constexpr int kWideRows = 32;                         // rows of a workgroup whe
 struct Kv4Plan {
   int group;             // query heads of a key/value head
   int rows;              // requests * fresh * group: rows of a key/value head
-  int own_rows;          // rows of a workgroup on a request's own keys: 4, 8, 16 or 32
+  int own_rows;          // rows of a workgroup on a request's own keys: 8, 16 or 32
   bool share;            // whether the prefix is taken for all requests at once
   int prefix_tiles, prefix_parts;
   int own_tiles, own_parts;
@@ -87,13 +102,13 @@ void choose_shared_parts(Kv4Plan& p, int64_t requests, int kv_heads, int64_t pre
   }
 }
 
-Kv4Plan make_kv4_plan(int64_t requests, int fresh, int q_heads, int kv_heads, int head_dim, int64_t max_len, int64_t prefix, bool split) {
+Kv4Plan make_kv4_plan(int64_t requests, int fresh, int q_heads, int kv_heads, int64_t max_len, int64_t prefix, bool split) {
   Kv4Plan p = {};
   p.group = q_heads / kv_heads;
   p.rows = (int)(requests * fresh * p.group);
   p.line_rows = requests * fresh * q_heads;
   const int64_t mine = (int64_t)fresh * p.group;
-  p.own_rows = mine <= 4 && head_dim == 128 ? 4 : mine <= 8 ? 8 : mine <= 16 ? 16 : kWideRows;
+  p.own_rows = mine <= 8 ? 8 : mine <= 16 ? 16 : kWideRows;
   p.own_tiles = (int)ceil_div(mine, p.own_rows);
   p.own_parts = 1;
   if (!split) return p;
@@ -107,19 +122,20 @@ Kv4Plan make_kv4_plan(int64_t requests, int fresh, int q_heads, int kv_heads, in
   }
   // nothing is shared or split where a launch could not hold it: own_tiles alone fit one (checked before)
   if ((p.prefix_groups() + requests * p.own_tiles * p.own_parts) * kv_heads >= kMaxGroups || p.line_rows >= kJoinThreads / 64 * kMaxGroups)
-    return make_kv4_plan(requests, fresh, q_heads, kv_heads, head_dim, max_len, 0, false);
+    return make_kv4_plan(requests, fresh, q_heads, kv_heads, max_len, 0, false);
   return p;
 }
 
-// F column groups share a product's 16 columns: with few rows, column cg * (16 / F) + i of it is query i against the
-// head's groups cg * kSets ... cg * kSets + kSets - 1 alone (its operands are zero for the others).  So a chain of F
-// products leaves F groups' sums in one accumulator, each lane scales its own groups only, and the columns are
-// added up once they are scores; the weights are scaled likewise, and of an output tile the columns of its
-// own group count.
+// F = 2: two column groups share a product's 16 columns.  With up to 8 rows, column 8 cg + i of it is query i against
+// half of the head's groups of 32, cg * kSets ... cg * kSets + kSets - 1, alone (its operands are zero for the others).
+// So a chain of two products leaves two groups' sums in one accumulator, each lane scales its own groups only, and the
+// columns are added up once they are scores; the weights are scaled likewise, and of an output tile the columns of
+// its own groups count.  96 requests of 8192 keys, 4 or 5 rows: 158 us, 164 with F = 1 (four column groups for up to
+// 4 rows: 158 too, and not kept).
 template <int D, int F>
 struct Fold {
   static constexpr int kGroups = D / 32, kSets = kGroups / F, kRows = 16 / F;
-  static_assert(kGroups % F == 0 && (F == 1 || kSets <= 2), "a lane's groups share a word of scales");
+  static_assert(F == 1 || F == 2, "folded, a lane's groups share a word of scales");
 };
 
 // The scales of four keys, for the groups of a lane: binary16, where `of` finds them.
@@ -299,18 +315,14 @@ struct Kv4Rows {
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            s[rt][u][i] += turned<8>(s[rt][u][i]);
-            if constexpr (F == 4) s[rt][u][i] += turned<4>(s[rt][u][i]);
-          }
+          for (int i = 0; i < 4; ++i) s[rt][u][i] += other_half(s[rt][u][i]);
       }
     }
   }
 
-  // The value N columns further, round the 16.
-  template <int N>
-  static __device__ __forceinline__ float turned(float v) {
-    return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), 0x120 + N, 0xF, 0xF, true));
+  // The value 8 columns further, round the 16.
+  static __device__ __forceinline__ float other_half(float v) {
+    return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), 0x128, 0xF, 0xF, true));
   }
 
   // The values' codes of two halves, elements 16 t ... 16 t + 15, as an A operand.
@@ -585,7 +597,7 @@ __device__ __forceinline__ void walk_rows(const Decode<T>& a, const uint8_t* cac
 
 // SHARE: some workgroups take the prefix for all requests.
 template <typename T, int D, int RT, int F, bool SHARE>
-__global__ __launch_bounds__(kThreads, SHARE || RT > 1 ? 2 : F > 1 ? 4 : 3) void decode_kv4_kernel(const Decode<T> a, const uint8_t* cache, const Kv4Plan p, const Parts parts, int prefix_groups, bool sorted) {
+__global__ __launch_bounds__(kThreads, SHARE || RT > 1 ? 2 : F > 1 ? 4 : 3) void decode_kv4_kernel(const Decode<T> a, const uint8_t* cache, const Kv4Plan p, const Parts parts, int prefix_groups) {
   constexpr int kOwnRows = RT * 16 / F;
   __shared__ union {
     Shared<D, kOwnRows> own;
@@ -607,8 +619,7 @@ __global__ __launch_bounds__(kThreads, SHARE || RT > 1 ? 2 : F > 1 ? 4 : 3) void
   int i = turn - prefix_groups, part = i % p.own_parts;
   i /= p.own_parts;
   const int index0 = i % p.own_tiles * kOwnRows;
-  int request = i / p.own_tiles;
-  if (sorted) request = longest_first(a, request);
+  const int request = i / p.own_tiles;
   const int len = request_len(a, request), from = min(SHARE ? prefix : 0, len), base = from & ~(kTileKeys - 1);
   const int per = ((len - base + p.own_parts - 1) / p.own_parts + kStepKeys - 1) / kStepKeys * kStepKeys;
   const int lo = max(min(base + part * per, len), from), hi = min(base + (part + 1) * per, len);
@@ -623,20 +634,19 @@ template <typename T, int D, int RT, int F>
 hipError_t launch_kv4(const Decode<T>& a, const uint8_t* cache, const Kv4Plan& p, const Parts& parts, hipStream_t stream) {
   const int64_t prefix_groups = p.prefix_groups(), own_groups = a.requests * p.own_tiles * p.own_parts;
   const dim3 grid((unsigned)((prefix_groups + own_groups) * a.kv_heads));
-  if (p.share) decode_kv4_kernel<T, D, RT, F, true><<<grid, kThreads, 0, stream>>>(a, cache, p, parts, (int)prefix_groups, false);
-  else decode_kv4_kernel<T, D, RT, F, false><<<grid, kThreads, 0, stream>>>(a, cache, p, parts, 0, false);
+  if (p.share) decode_kv4_kernel<T, D, RT, F, true><<<grid, kThreads, 0, stream>>>(a, cache, p, parts, (int)prefix_groups);
+  else decode_kv4_kernel<T, D, RT, F, false><<<grid, kThreads, 0, stream>>>(a, cache, p, parts, 0);
   if (p.parts() > 1) launch_join<T, D>(a, p.line_rows, p.parts(), parts, stream);
   return hipGetLastError();
 }
 
 template <typename T, int D>
 hipError_t launch_kv4_dim(const Decode<T>& a, const uint8_t* cache, void* workspace, size_t workspace_bytes, hipStream_t stream) {
-  Kv4Plan p = make_kv4_plan(a.requests, a.fresh, a.q_heads, a.kv_heads, D, a.max_len, a.prefix, true);
+  Kv4Plan p = make_kv4_plan(a.requests, a.fresh, a.q_heads, a.kv_heads, a.max_len, a.prefix, true);
   const size_t need = parts_bytes(p.parts(), p.line_rows, D);
-  if (need > 0 && (workspace == nullptr || workspace_bytes < need)) p = make_kv4_plan(a.requests, a.fresh, a.q_heads, a.kv_heads, D, a.max_len, a.prefix, false);
+  if (need > 0 && (workspace == nullptr || workspace_bytes < need)) p = make_kv4_plan(a.requests, a.fresh, a.q_heads, a.kv_heads, a.max_len, a.prefix, false);
   const Parts parts = p.parts() > 1 ? place_parts<D>(workspace, p.parts(), p.line_rows) : Parts{nullptr, nullptr};
   switch (p.own_rows) {
-    case 4: if constexpr (D == 128) return launch_kv4<T, D, 1, 4>(a, cache, p, parts, stream);
     case 8: return launch_kv4<T, D, 1, 2>(a, cache, p, parts, stream);
     case 16: return launch_kv4<T, D, 1, 1>(a, cache, p, parts, stream);
     default: return launch_kv4<T, D, 2, 1>(a, cache, p, parts, stream);
@@ -647,7 +657,7 @@ hipError_t launch_kv4_dim(const Decode<T>& a, const uint8_t* cache, void* worksp
 }  // namespace attention
 
 size_t attention_decode_kv4_workspace_bytes(int64_t requests, int fresh, int q_heads, int kv_heads, int head_dim, int64_t max_len, int64_t prefix) {
-  const attention::Kv4Plan p = attention::make_kv4_plan(requests, fresh, q_heads, kv_heads, head_dim, max_len, prefix, true);
+  const attention::Kv4Plan p = attention::make_kv4_plan(requests, fresh, q_heads, kv_heads, max_len, prefix, true);
   return attention::parts_bytes(p.parts(), p.line_rows, head_dim);
 }
 

@@ -38,19 +38,6 @@ __device__ __forceinline__ int request_len(const Decode<T>& a, int request) {
   return (int)min((int64_t)max(a.lens[request], 0), room);
 }
 
-// The request that takes place `i` where those of each 64 stand longest first, so that what starts
-// last is short.
-template <typename T>
-__device__ __forceinline__ int longest_first(const Decode<T>& a, int i) {
-  const int lane = threadIdx.x & 63, base = i & ~63, r = base + lane;
-  const bool there = r < a.requests;
-  const uint32_t key = (there ? (uint32_t)(min(max(a.lens[there ? r : base], 0), (1 << 25) - 1) + 1) << 6 : 0u) | (uint32_t)(63 - lane);
-  int before = 0;
-#pragma unroll 16
-  for (int j = 0; j < 64; ++j) before += (uint32_t)__builtin_amdgcn_readlane((int)key, j) > key ? 1 : 0;
-  return base + __builtin_ctzll(__builtin_amdgcn_ballot_w64(before == (i & 63)));
-}
-
 // Four consecutive outputs of a row, of one part or of all.
 template <typename T, int D>
 __device__ __forceinline__ void put(const Decode<T>& a, int64_t line_rows, const Parts& parts, int part, const Row& row,

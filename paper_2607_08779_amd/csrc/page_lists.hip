@@ -4,9 +4,10 @@
 //
 // Fork, collect and compact move a few bytes for each table entry and page, so that launches and latency
 // bound them.  Fork is one launch: every workgroup finds for itself how many pages the rows before its
-// own take, as page_tables.hip does.  Collect and compact mark held pages with plain byte stores
-// (any order gives the same marks), count them for each block of pages, and write lists whose
-// places follow from the counts.  A copy is bound by the pages' bytes, read and written.
+// own take, as page_tables.hip does (64 rows 3.9 us, 1024 rows of 512 pages 5.7).  Collect and compact mark held
+// pages, count them and write lists whose places follow from the counts (64 requests, 9000 pages 8.6 us;
+// compacting 98000 pages of 512 requests 13.6).  A copy is bound by the pages' bytes, read and written (939 MB 165 us,
+// 5.7 TB/s).  Nothing depends on the order in which workgroups or atomics run.
 #include "page_lists.h"
 
 namespace ssq {
@@ -318,9 +319,9 @@ __global__ __launch_bounds__(kThreads) void rename_kernel(const PageCollect a, c
 
 // Pools of up to 131072 pages: every workgroup has all marks, in bits in LDS, and counts them for itself; then each takes
 // its share of the lists and rows.  The marks of a small table every workgroup makes for itself, in the only launch
-// (64 requests, 9000 pages: 10.4 us in the launches above, 5.8 so).  Where the table is larger, atomics on LDS at
+// (64 requests, 9000 pages: 10.4 us in the launches above, 8.6 so).  Where the table is larger, atomics on LDS at
 // random places would take longer than marking in memory in launches of its own (compacting 98000 pages of 512
-// requests: 31 us in the launches above, 46 in one, 14 in three).
+// requests: 31 us in the launches above, 46 in one, 13.6 in three).
 constexpr int kOneThreads = 1024, kOneWaves = kOneThreads / 64;
 constexpr int kOnePages = 1 << 17, kOneWords = kOnePages / 32, kOneRows = 2048;
 constexpr int64_t kOneEntries = 1 << 14;          // of a table that every workgroup marks for itself

@@ -168,6 +168,11 @@ DECODES = [
     ([31, 32, 33, 15, 16, 17, 47, 48, 49], 1, 15, 16, (4, 2, 64)),
     ([127, 128, 129, 255, 256, 257], 1, 0, 32, (3, 3, 128)),
     ([520, 470], 6, 300, 16, (20, 4, 128)),                # 30 rows a key/value head
+    ([90, 100, 95], 3, 64, 16, (16, 4, 128)),              # 12 rows
+    ([2900], 1, 0, 64, (16, 1, 128)),                      # 16 rows, in parts
+    ([2500, 1700], 4, 0, 32, (10, 2, 128)),                # 20 rows, in parts
+    ([1900, 2300], 3, 0, 16, (12, 6, 64)),                 # 6 rows, in parts
+    ([350 + 11 * i for i in range(33)], 1, 333, 32, (7, 1, 128)),
 ]
 
 
@@ -293,6 +298,23 @@ def test_decode_values_that_are_nan_reach_the_rows_that_see_them(dtype):
     out = run(q, cache, table, [n], 0)[0]                                # positions 92..99
     assert out[:3].isfinite().all() and out[3:, 2:].isnan().all() and out[:5, :2].isfinite().all()
     assert out[5:, :2, 32:].isnan().all() and out[5:, :2, :32].isfinite().all()
+
+
+def test_decode_of_as_many_requests_as_a_launch_holds():
+    """2^20 requests of 15 heads, a workgroup each: those of no token give zeros, of one token its value."""
+    n, heads, d, page = 1 << 20, 15, 64, 16
+    g = gen(675)
+    k, v = (torch.randn((4 * page, heads, d), generator=g, device="cuda").bfloat16() for _ in "kv")
+    cache = new_cache(4, heads, page, d)
+    _, held = ssq.ssq_kv4_store(k, v, torch.arange(4 * page, device="cuda", dtype=torch.int32), cache, held=True)
+    q = torch.randn((n, 1, heads, d), generator=g, device="cuda", dtype=BF)
+    request = torch.arange(n, device="cuda", dtype=torch.int32)
+    lens, table = request % 2, (request % 4)[:, None].contiguous()
+    out = ssq.ssq_attention_decode_kv4(q, cache, table, lens, page)
+    assert not out[::2].any()
+    for r in (1, 3):                               # weight times scale, and the quotient, rounded once each
+        want = held[page * r].float()
+        assert ((out[r::4, 0].float() - want).abs() <= 2.0 ** -7 * want.abs()).all()
 
 
 # --- a row is a function of what it sees ----------------------------------------------------------

@@ -9,7 +9,10 @@ their own, and are answered token by token.  Every step is
     ssq_attention_prompt / _decode          over the prompt, or over the cache with its shared prefix
     ssq_matmul (o)
 
-    python examples/attention_layer.py [--users 16] [--system 2048] [--own 4] [--tokens 32]
+With --kv4 the cache holds 4 bits an element: ssq_kv4_store follows ssq_qk_norm_rope, the prompt attends to
+its rows as the cache holds them, and ssq_attention_decode_kv4 reads them.
+
+    python examples/attention_layer.py [--users 16] [--system 2048] [--own 4] [--tokens 32] [--kv4]
 """
 import argparse
 import os
@@ -28,7 +31,7 @@ PAGE, GROUP, BITS = 64, 32, 4
 class Layer:
     """Quantized projections, gains of the head norms, and this layer's cache."""
 
-    def __init__(self, hidden=4096, q_heads=32, kv_heads=8, head_dim=128, pages=256, seed=0):
+    def __init__(self, hidden=4096, q_heads=32, kv_heads=8, head_dim=128, pages=256, seed=0, kv4=False):
         self.hidden, self.q_heads, self.kv_heads, self.head_dim = hidden, q_heads, kv_heads, head_dim
         g = torch.Generator(device="cuda").manual_seed(seed)
         rows = {"q": q_heads * head_dim, "k": kv_heads * head_dim, "v": kv_heads * head_dim, "o": hidden}
@@ -38,16 +41,23 @@ class Layer:
             w = (torch.randn((n, cols[name]), generator=g, device="cuda") * 0.02).bfloat16()
             self.weights[name] = (n, cols[name], *ssq.ssq_quantize(w, GROUP, BITS, ssq.SIGNED_SYM)[:2])
         self.q_gain, self.k_gain = ((1 + 0.1 * torch.randn(head_dim, generator=g, device="cuda")).bfloat16() for _ in "qk")
-        shape = (pages, kv_heads, PAGE, head_dim)
-        self.k_pages, self.v_pages = (torch.zeros(shape, dtype=torch.bfloat16, device="cuda") for _ in "kv")
+        self.pages, self.cache = pages, None
+        if kv4:
+            self.cache = ssq.ssq_kv4_cache(pages, kv_heads, PAGE, head_dim)
+        else:
+            shape = (pages, kv_heads, PAGE, head_dim)
+            self.k_pages, self.v_pages = (torch.zeros(shape, dtype=torch.bfloat16, device="cuda") for _ in "kv")
 
     def project(self, name, x):
         n, k, codes, scales = self.weights[name]
         return ssq.ssq_matmul(x, codes, scales, None, n, k, GROUP, BITS)
 
     def qkv(self, x, positions, slots, rope):
-        """q, k (normed, rotated) and v [tokens, heads, head_dim]; k and v are in the cache then."""
+        """q, k (normed, rotated) and v [tokens, heads, head_dim]; k and v are in the cache then (and, in 4 bits, what it holds)."""
         q, k, v = (self.project(n, x).view(len(x), -1, self.head_dim) for n in "qkv")
+        if self.cache is not None:
+            q, k = ssq.ssq_qk_norm_rope(q, k, positions, rope, q_gain=self.q_gain, k_gain=self.k_gain)
+            return q, *ssq.ssq_kv4_store(k, v, slots, self.cache, held=(k, v))
         q, k = ssq.ssq_qk_norm_rope(q, k, positions, rope, q_gain=self.q_gain, k_gain=self.k_gain, v=v, slots=slots,
                                     k_pages=self.k_pages, v_pages=self.v_pages)
         return q, k, v
@@ -62,9 +72,10 @@ class Layer:
 
     def decode(self, x, fresh, step, table, max_len, prefix, rope):
         """The last `fresh` tokens of every request: x [requests * fresh, hidden]."""
-        q, _, _ = self.qkv(x, step.positions, step.slots, rope)
-        return self.out(ssq.ssq_attention_decode(q.view(-1, fresh, self.q_heads, self.head_dim), self.k_pages, self.v_pages,
-                                                 table, step.lens, max_len, prefix=prefix))
+        q = self.qkv(x, step.positions, step.slots, rope)[0].view(-1, fresh, self.q_heads, self.head_dim)
+        if self.cache is not None:
+            return self.out(ssq.ssq_attention_decode_kv4(q, self.cache, table, step.lens, max_len, prefix=prefix))
+        return self.out(ssq.ssq_attention_decode(q, self.k_pages, self.v_pages, table, step.lens, max_len, prefix=prefix))
 
 
 class Step:
@@ -89,7 +100,7 @@ def serve(layer, system, users, own, tokens, inputs, seen=None):
     i32 = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
     max_len = system + own + tokens
     rope = rope_table(max_len, layer.head_dim)
-    free = torch.arange(layer.k_pages.shape[0], dtype=torch.int32, device="cuda")
+    free = torch.arange(layer.pages, dtype=torch.int32, device="cuda")
     width = -(-max_len // PAGE)
 
     table = torch.full((1, width), -1, dtype=torch.int32, device="cuda")
@@ -117,9 +128,10 @@ def main():
     ap.add_argument("--system", type=int, default=2048)
     ap.add_argument("--own", type=int, default=4)
     ap.add_argument("--tokens", type=int, default=32)
+    ap.add_argument("--kv4", action="store_true", help="a cache in 4 bits")
     a = ap.parse_args()
     pages = a.system // PAGE + a.users * (-(-(a.own + a.tokens) // PAGE))
-    layer = Layer(pages=pages)
+    layer = Layer(pages=pages, kv4=a.kv4)
     gen = torch.Generator(device="cuda").manual_seed(1)
     inputs = lambda n: torch.randn((n, layer.hidden), generator=gen, device="cuda").bfloat16()  # noqa: E731
     serve(layer, a.system, a.users, a.own, 2, inputs)              # the first calls load and allocate

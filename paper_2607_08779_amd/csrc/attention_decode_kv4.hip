@@ -82,9 +82,8 @@ int choose_parts(int64_t groups, int64_t keys, int64_t line_rows) {
 
 // The same beside a prefix, whose workgroups take 1.3 for a step of 128 keys and 32 rows, 2.3 where a CU has two of
 // them, and in between where it has work on own keys too; a CU that is full does a step in 1.15, one of a
-// request's own keys in 0.8.  Together: the work, or the longest workgroup.  64 requests of one key behind 8192 (256 rows, 8 key/value heads): 4 parts 32.3 us, 8 parts 32.8, 16
-// parts 40.0; behind 16384: 50.8, 45.0, 52.4; of 1 to 1024 keys behind 8192: 34.8 with 4 parts and 1, 40.6 with 3
-// and 1, 40.8 with 8 and 1.
+// request's own keys in 0.8.  Together: the work, or the longest workgroup.  64 requests of one key behind 8192 (256 rows, 8 key/value heads): 4 parts 31.7 us, 6 parts 34.2, 8
+// parts 31.9; behind 16384: 50.8, 54.1, 44.2; of 1 to 1024 keys behind 8192, undivided: 34.5, 37.9, 40.1.
 void choose_shared_parts(Kv4Plan& p, int64_t requests, int kv_heads, int64_t prefix, int64_t behind) {
   const int64_t wide = (int64_t)p.prefix_tiles * kv_heads, own = requests * p.own_tiles * kv_heads;
   double best_us = 0.0;
@@ -96,7 +95,7 @@ void choose_shared_parts(Kv4Plan& p, int64_t requests, int kv_heads, int64_t pre
       const double wide_us = 1.15 * wide_steps * (double)(wide * n) / 256.0, own_us = 0.8 * own_steps * (double)(own * m) / 256.0;
       const double pace = wide * n > 256 ? 2.3 : 1.3 + 0.6 * std::min(1.0, own_us / wide_us), all = wide_us + own_us;
       const double longest = std::max(wide_steps * pace, own_steps * 1.5);
-      const double us = std::max(all, longest) + 0.5e-3 * (double)((n + m) * p.line_rows);
+      const double us = std::max(all, longest) + 0.25e-3 * (double)((n + m) * p.line_rows);
       if ((n == 1 && m == 1) || us < best_us) p.prefix_parts = n, p.own_parts = m, best_us = us;
     }
   }

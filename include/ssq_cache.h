@@ -130,7 +130,8 @@ int ssq_page_fork(const int32_t* parents, int64_t requests, const int32_t* lens,
  * that have ended are left out, or have the length 0.  The list is one for ssq_page_tables and
  * ssq_page_fork, from entry 0 on.
  *
- *   lens        device, int32 [requests]; negative values count as 0
+ *   lens        device, int32 [requests]; negative values count as 0.  lens and table may be NULL if
+ *               requests or table_stride is 0
  *   table       device, int32 [requests, table_stride]; entries outside [0, pages) name none;
  *               requests * ceil(table_stride / 1024) < 2^24
  *   pages       pages of the pool; pages * page_size < 2^31

@@ -67,6 +67,7 @@ int collect(const int32_t* lens, int64_t requests, const int32_t* table, int64_t
       pages > INT32_MAX / page_size || requests * ((table_stride + 1023) / 1024) >= ssq::kMaxGroups)
     return SSQ_EINVAL;
   const bool rows = requests > 0 && table_stride > 0;
+  if (!rows) requests = 0;                 // of rows without entries not even the lengths are read: lens may be null
   if (count == nullptr || (pages > 0 && free_pages == nullptr) || (rows && (lens == nullptr || table == nullptr)) || workspace == nullptr ||
       workspace_bytes < ssq::page_collect_workspace_bytes(pages, compact))
     return SSQ_EINVAL;

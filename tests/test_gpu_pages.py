@@ -135,6 +135,23 @@ COPIES = [
 ]
 
 
+def test_rows_without_entries_need_no_lengths():
+    """Null lens and table where the table has no columns: every page is free."""
+    lib, pages = ssq.lib(), 40
+    for compact in (False, True):
+        need = ssq.ssq_page_collect_workspace_size(pages, compact)
+        ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+        free, count, src, dst, moved = (torch.full((n,), 55, dtype=torch.int32, device="cuda") for n in (pages, 1, pages // 2, pages // 2, 1))
+        stream = torch.cuda.current_stream().cuda_stream
+        if compact:
+            st = lib.ssq_page_compact(None, 5, None, 0, 16, pages, None, None, free.data_ptr(), count.data_ptr(), src.data_ptr(), dst.data_ptr(),
+                                      moved.data_ptr(), ws.data_ptr(), need, stream)
+            assert moved.tolist() == [0] and set(src.tolist() + dst.tolist()) == {-1}
+        else:
+            st = lib.ssq_page_collect(None, 5, None, 0, 16, pages, None, free.data_ptr(), count.data_ptr(), ws.data_ptr(), need, stream)
+        assert st == 0 and free.tolist() == list(range(pages)) and count.tolist() == [pages]
+
+
 @pytest.mark.parametrize("i", range(len(COPIES)))
 def test_copy(i):
     count, pages, size, entries = COPIES[i]

@@ -372,7 +372,7 @@ __global__ __launch_bounds__(kOneThreads) void pool_kernel(const PageCollect a, 
   __shared__ OneLds lds;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int pages = (int)a.pages, words = (pages + 31) / 32, rows = (int)a.requests, stride = (int)a.stride;
-  const int stretches = (stride + 63) / 64, tasks = rows * stretches;
+  const int stretches = (int)((a.stride + 63) / 64), tasks = rows * stretches;
   for (int r = tid; r < rows; r += kOneThreads) lds.row_pages[r] = min(pages_of(a.lens[r], a.shift), (uint32_t)stride);
   if constexpr (MARKED) {
     // 16 marks of a byte each to two bits; what lies behind the pages is marked as held

@@ -152,6 +152,19 @@ def test_rows_without_entries_need_no_lengths():
         assert st == 0 and free.tolist() == list(range(pages)) and count.tolist() == [pages]
 
 
+def test_compact_the_widest_row():
+    width, pages = 2 ** 31 - 1, 100
+    if torch.cuda.mem_get_info()[0] < 5 * width:
+        pytest.skip("needs 10 GB of device memory")
+    table = torch.full((1, width), -1, dtype=torch.int32, device="cuda")
+    table[0, :4] = ints([90, 5, 99, 7])
+    out = [table, *(torch.full((n,), 55, dtype=torch.int32, device="cuda") for n in (pages, 1, pages // 2, pages // 2, 1))]
+    _, free, count, src, dst, moved = ssq.ssq_page_compact(ints([33]), table, 16, pages, out=out)
+    assert table[0, :4].tolist() == [1, 0, 2, 7] and int(table[0, -1]) == -1       # entry 3 is behind the row's pages
+    assert free.tolist() == list(range(3, 100)) + [-1] * 3 and count.tolist() == [97]
+    assert src.tolist()[:4] == [5, 90, 99, -1] and dst.tolist()[:4] == [0, 1, 2, -1] and moved.tolist() == [3]
+
+
 @pytest.mark.parametrize("i", range(len(COPIES)))
 def test_copy(i):
     count, pages, size, entries = COPIES[i]

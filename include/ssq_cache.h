@@ -68,7 +68,8 @@ int ssq_kv4_store_f32(const float* k, int64_t k_stride, const float* v, int64_t 
  * requests * (fresh * q_heads + 16 kv_heads) < 2^28.
  * Codes enter the products exactly and scales in binary32.  In bf16, weight times value scale is
  * rounded to bf16 for the product with the codes, each of a row's D/32 groups for itself; the sum that
- * divides them is that of the unrounded weights.  In binary32 nothing is rounded to fewer bits.
+ * divides them is that of the unrounded weights.  Codes enter bf16 products with an offset that is taken
+ * out again in binary32: queries of magnitude 2^114 and above may overflow there and give NaN.  In binary32 nothing is rounded to fewer bits.
  */
 int ssq_attention_decode_kv4(const uint16_t* q, int64_t q_stride, int64_t requests, int fresh,
                              int q_heads, int kv_heads, int head_dim, float scale, const uint8_t* cache,

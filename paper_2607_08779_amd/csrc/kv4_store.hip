@@ -45,12 +45,20 @@ struct Eight<uint16_t> {
     *positive = max((int)s[0], (int)s[1]);
   }
   static __device__ __forceinline__ float value(uint32_t bits) { return __uint_as_float(bits << 16); }
-  // With M and w of 8 significant bits w / s = 8 w / M is a half-integer, or at least 2^-11 from every one; w times the
+  // c = rne(fl32(w / s)) + 8 in a float's lowest bits.  With M and w of 8 significant bits w / s = 8 w / M is a half-integer, or at least 2^-11 from every one; w times the
   // reciprocal of s is within 2^-18 of it.  Rounded to a multiple of 2^-13 (the spacing about 1.5 * 2^10) it is the
   // half-integer again in the first case and on the same side in the second, so that rounding it to even gives
   // rne(fl32(w / s)).  Outside the range of s where the reciprocal is that close, divide.
-  static __device__ __forceinline__ bool near(float most) { return most >= 0x1p-100f && most <= 0x1p100f; }
-  static __device__ __forceinline__ float rounded(float w, float by) { return __builtin_fmaf(w, by, 0x1.8p10f) + (kRound - 0x1.8p10f); }
+  __device__ __forceinline__ void over(float s, float most, float (&c)[8]) const {
+    if (most >= 0x1p-100f && most <= 0x1p100f) {
+      const float by = __builtin_amdgcn_rcpf(s);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) c[i] = __builtin_fmaf(of(i), by, 0x1.8p10f) + (kRound - 0x1.8p10f);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) c[i] = of(i) / s + kRound;
+    }
+  }
   static __device__ __forceinline__ void store(uint16_t* p, const float (&w)[8]) {
     *reinterpret_cast<u32x4*>(p) = u32x4{pack_bf16x2(w[0], w[1]), pack_bf16x2(w[2], w[3]), pack_bf16x2(w[4], w[5]), pack_bf16x2(w[6], w[7])};
   }
@@ -74,16 +82,17 @@ struct Eight<float> {
     }
   }
   static __device__ __forceinline__ float value(uint32_t bits) { return __uint_as_float(bits); }
-  static __device__ __forceinline__ bool near(float) { return false; }
-  static __device__ __forceinline__ float rounded(float, float) { return kRound; }
+  __device__ __forceinline__ void over(float s, float, float (&c)[8]) const {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) c[i] = of(i) / s + kRound;
+  }
   static __device__ __forceinline__ void store(float* p, const float (&w)[8]) {
     *reinterpret_cast<f32x4*>(p) = f32x4{w[0], w[1], w[2], w[3]};
     *reinterpret_cast<f32x4*>(p + 4) = f32x4{w[4], w[5], w[6], w[7]};
   }
 };
 
-// The codes of 8 elements (+ 8, lowest first) and their group's scale in binary16; `held`, where
-// wanted: what they stand for.  A
+// The codes of 8 elements (+ 8, lowest first) and their group's scale in binary16; `held`, where wanted: what they stand for.  A
 // group that holds an infinity or a NaN, or whose scale binary16 does not reach, has codes 8 and the scale NaN, so
 // that all of it reads as NaN.
 template <typename T>
@@ -108,13 +117,8 @@ __device__ __forceinline__ uint32_t on_grid(const Eight<T>& x, uint32_t* scale, 
   if (size == 0 || bits == 0x7E00u) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) c[i] = kRound;
-  } else if (E::near(most)) {
-    const float inverse = __builtin_amdgcn_rcpf(s);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) c[i] = E::rounded(x.of(i), inverse);
   } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) c[i] = x.of(i) / s + kRound;
+    x.over(s, most, c);
   }
 #pragma unroll
   for (int i = 0; i < 8; ++i) c[i] = fminf(c[i], kRound + 7.0f);

@@ -5,8 +5,8 @@
 // Fork, collect and compact move a few bytes for each table entry and page, so that launches and latency
 // bound them.  Fork is one launch: every workgroup finds for itself how many pages the rows before its
 // own take, as page_tables.hip does (64 rows 3.9 us, 1024 rows of 512 pages 5.7).  Collect and compact mark held
-// pages, count them and write lists whose places follow from the counts (64 requests, 9000 pages 8.6 us;
-// compacting 98000 pages of 512 requests 13.6).  A copy is bound by the pages' bytes, read and written (939 MB 165 us,
+// pages, count them and write lists whose places follow from the counts (64 requests, 9000 pages 8.7 us;
+// compacting 98000 pages of 512 requests 13.7).  A copy is bound by the pages' bytes, read and written (939 MB 165 us,
 // 5.7 TB/s).  Nothing depends on the order in which workgroups or atomics run.
 #include "page_lists.h"
 

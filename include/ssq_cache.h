@@ -14,6 +14,7 @@
  * head, one binary16 scale each.  For groups w of a row,
  *   M = max|w|;  s = -M / 8 if max w > -min w, else M / 8   (binary32; +0 if M = 0)
  *   c = clip(rne(fl32(w / s)), -8, 7), 0 if M = 0;  held value = c * binary16(s).
+ * (In binary32 rows of M <= 2^-147, s rounds to zero; there w = 0 has c = -8, as in ssq_quantize_f32.)
  * A group that holds an infinity or a NaN, or whose s binary16 does not reach (M >= 524160), has the
  * codes c = 0 and the scale NaN: all of it reads as NaN.
  *   cache  uint8 [pages, kv_heads, 2, page_size * (D/2 + D/16)], D = head_dim: for each page

@@ -82,9 +82,11 @@ struct Eight<float> {
     }
   }
   static __device__ __forceinline__ float value(uint32_t bits) { return __uint_as_float(bits); }
+  // Where s is below the normal numbers, rounded or zero, quotients go below -8 too; 0 / 0 counts as -8, as in
+  // ssq_quantize_f32.  (In bf16 M / 8 is exact, and no quotient is below -8.)
   __device__ __forceinline__ void over(float s, float, float (&c)[8]) const {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) c[i] = of(i) / s + kRound;
+    for (int i = 0; i < 8; ++i) c[i] = fmaxf(of(i) / s + kRound, kRound - 8.0f);
   }
   static __device__ __forceinline__ void store(float* p, const float (&w)[8]) {
     *reinterpret_cast<f32x4*>(p) = f32x4{w[0], w[1], w[2], w[3]};

@@ -113,6 +113,37 @@ def test_store_of_odd_groups(dtype):
     assert held[0][8].isfinite().all()
 
 
+def test_store_of_groups_near_the_smallest_numbers():
+    """Binary32 groups whose scale is below the normal numbers, rounded or zero: quotients beyond both ends of the grid
+    are clipped, every code is that of ssq_quantize_f32, and what is held is zero, as binary16 has no such scale."""
+    dim, page, heads, tokens = 64, 64, 2, 128
+    g = torch.Generator().manual_seed(640)
+    tiny = 2.0 ** -149
+    size = torch.tensor([*range(1, 101), *(1 << n for n in range(7, 32)), 3, 11, 12], dtype=torch.float64)
+    k = torch.rand((tokens, heads, dim), generator=g, dtype=torch.float64) * 2 - 1
+    k[:, 1] = k[:, 1].sign() * (torch.rand((tokens, dim), generator=g) < 0.3)      # ends of the grid, and zeros
+    k[:, :, 7], k[:, :, 40] = 1.0, -1.0                                    # the largest of their groups
+    k = ((k * size[:, None, None]).round() * tiny).float()
+    assert (k[:, :, 7].double() == size[:, None] * tiny).all()
+    rows = k.cuda(), (-k).cuda()
+    cache = new_cache(2, heads, page, dim)
+    held = ssq.ssq_kv4_store(*rows, torch.arange(tokens, device="cuda", dtype=torch.int32), cache, held=True)
+    for x, h, (u, s) in zip(rows, held, Q.read(cache, page, dim)):
+        assert (h == 0).all() and (s == 0).all()
+        codes, scales, _ = ssq.ssq_quantize(x.reshape(tokens * heads, dim), 32, 4, ssq.SIGNED_SYM)
+        codes = codes.cpu().view(tokens, heads, dim // 2)
+        got = u.permute(0, 2, 1, 3).reshape(tokens, heads, dim)
+        assert torch.equal(got, torch.stack((codes & 15, codes >> 4), -1).flatten(2).to(torch.int32))
+        assert torch.equal(bits(s.permute(0, 2, 1, 3).reshape(tokens * heads, 2).half()), scales.cpu())
+        # and the definition, wherever the quotient is a number: s as binary32 rounds it
+        w = x.cpu().double().unflatten(2, (-1, 32))
+        hi, down = w.amax(3, keepdim=True), -w.amin(3, keepdim=True)
+        step = (torch.maximum(hi, down) / 8).float().double()
+        c = (w / torch.where(hi > down, -step, step)).float().round().clamp(-8, 7)
+        known = ~c.isnan()
+        assert torch.equal(got.unflatten(2, (-1, 32))[known], (c[known] + 8).to(torch.int32))
+
+
 @pytest.mark.parametrize("dtype", [BF, F32])
 def test_store_in_place_and_into_strided_rows(dtype):
     t, heads, dim, page = 29, 3, 64, 16

@@ -76,8 +76,9 @@ int collect(const int32_t* lens, int64_t requests, const int32_t* table, int64_t
     if (!aligned(p, 4)) return SSQ_EALIGN;
   if (!aligned(workspace, 256)) return SSQ_EALIGN;
   const int64_t entries = requests * table_stride, half = compact ? pages / 2 : 0;
+  const bool in_place = compact && table_out == table;      // one array, which is written
   const Span arrays[] = {{free_pages, pages}, {count, 1}, {src, half}, {dst, half}, {moved, compact}, {workspace, (int64_t)workspace_bytes, 1},
-                         {table_out, compact && table_out != table ? entries : 0}, {lens, requests}, {table, entries}, {pinned, pinned != nullptr ? pages : 0, 1}};
+                         {table_out, compact ? entries : 0}, {lens, requests}, {table, in_place ? 0 : entries}, {pinned, pinned != nullptr ? pages : 0, 1}};
   if (!separate(arrays, 7)) return SSQ_EINVAL;
   const ssq::PageCollect a = {lens, table, pinned, table_out, free_pages, count, src, dst, moved, requests, table_stride, pages, shift_of(page_size)};
   return status_of(ssq::launch_page_collect(a, compact, workspace, stream));

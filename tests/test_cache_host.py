@@ -157,6 +157,14 @@ def test_collect_and_compact_refuse_outputs_over_other_arrays(written, other):
         assert call("ssq_page_collect", COLLECT, {which: off((50 << 20) + n)}) == EALIGN == call("ssq_page_compact", COMPACT, {which: off((50 << 20) + n)})
 
 
+@pytest.mark.parametrize("other", ["lens", "pinned", "free_pages", "count", "src", "dst", "moved", "workspace"])
+def test_compact_in_place_refuses_other_arrays_in_the_table(other):
+    """Where the table is renamed in place, it is written while other workgroups still read lengths and pins."""
+    here, size = COMPACT["table"].value, POOL_BYTES[other]
+    for first in (here, here - size + 256) if other == "workspace" else (here, here + 16, here + POOL_BYTES["table"] - 4, here - size + 4 & ~3):
+        assert call("ssq_page_compact", COMPACT, {"table_out": COMPACT["table"], other: ctypes.c_void_p(first)}) == EINVAL, (other, first)
+
+
 def copy(caches, page_bytes=1152, pages=5, src=at(20), dst=at(21), entries=3, count=None):
     pointers = (ctypes.c_void_p * max(len(caches), 1))(*(c.value if c else None for c in caches)) if caches is not None else None
     return ssq.lib().ssq_page_copy(pointers, len(caches or ()) if count is None else count, page_bytes, pages, src, dst, entries, None)

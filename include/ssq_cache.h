@@ -50,7 +50,9 @@ extern "C" {
  *                   slots stay as they are.
  *   cache, pages, page_size   the cache; at most 2^31 - 1 slots
  *   k_held, v_held  device, bf16, written, or NULL; may be k and v themselves with their
- *                   strides (no other array that is written may overlap one that is read)
+ *                   strides, and where k and v are the same rows, the same rows too
+ * No other array that is written, the cache among them, may overlap another argument's.  Rows may lie
+ * between those of another array, as in the rows of one projection.
  */
 int ssq_kv4_store(const uint16_t* k, int64_t k_stride, const uint16_t* v, int64_t v_stride,
                   int64_t tokens, int kv_heads, int head_dim, const int32_t* slots, uint8_t* cache,

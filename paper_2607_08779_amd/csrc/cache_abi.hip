@@ -2,6 +2,8 @@
 // include/ssq_cache.h).  Every check runs on the host before any HIP call.
 #include "ssq_cache.h"
 
+#include <algorithm>
+
 #include "attention_checks.h"
 #include "kv4.h"
 #include "page_lists.h"
@@ -17,6 +19,30 @@ bool separate(const Span (&arrays)[N], int written) {
     for (int j = i + 1; j < N; ++j)
       if (overlap(arrays[i], arrays[j])) return false;
   return true;
+}
+
+// `count` rows of `bytes` bytes, `stride` bytes apart; no rows: an array that is not given.
+struct RowSpan {
+  const void* p;
+  int64_t count, bytes, stride;
+};
+bool same(const RowSpan& a, const RowSpan& b) { return a.p == b.p && a.stride == b.stride; }
+// Whether a byte is in a row of both.  Not by their ends alone: k and v lie between each other in the rows of a fused
+// projection, as may the rows that are written.
+bool overlap(const RowSpan& a, const RowSpan& b) {
+  if (a.count == 0 || b.count == 0) return false;
+  const int64_t d = (int64_t)(reinterpret_cast<uintptr_t>(b.p) - reinterpret_cast<uintptr_t>(a.p));
+  if (d >= (a.count - 1) * a.stride + a.bytes || -d >= (b.count - 1) * b.stride + b.bytes) return false;
+  if (a.count > b.count) return overlap(b, a);
+  // whether a row of a that begins `at` bytes behind b's first one meets the first of b's rows, from `from` on, that ends behind `at`
+  auto meets = [&](int64_t at, int64_t from) {
+    const int64_t x = at - b.bytes, floor = x / b.stride - (x % b.stride < 0), j = std::max(floor + 1, from);
+    return j < b.count && j * b.stride < at + a.bytes;
+  };
+  if (a.stride == b.stride) return meets(-d, 1 - a.count);        // the difference of two rows' numbers is what counts
+  for (int64_t i = 0; i < a.count; ++i)
+    if (meets(i * a.stride - d, 0)) return true;
+  return false;
 }
 
 template <typename T>
@@ -37,6 +63,19 @@ int kv4_store(const T* k, int64_t k_stride, const T* v, int64_t v_stride, int64_
   for (const void* p : {(const void*)k, (const void*)v, (const void*)cache, (const void*)k_held, (const void*)v_held})
     if (!aligned(p, 16)) return SSQ_EALIGN;
   if (!aligned(slots, 4)) return SSQ_EALIGN;
+  // Of rows that are written, a thread reads and writes the same elements of k, v and both outputs; so k_held may be k, and where
+  // k and v are the same rows all four may be.
+  auto rows = [&](const T* p, int64_t stride) { return RowSpan{p, p != nullptr ? tokens : 0, (int64_t)sizeof(T) * kv_heads * head_dim, (int64_t)sizeof(T) * stride}; };
+  const RowSpan kr = rows(k, k_stride), vr = rows(v, v_stride), kh = rows(k_held, k_held_stride), vh = rows(v_held, v_held_stride);
+  const int64_t cache_bytes = pages * kv_heads * page_size * (head_dim + head_dim / 8);
+  const RowSpan cached = {cache, cache_bytes > 0, cache_bytes, cache_bytes}, places = {slots, 1, 4 * tokens, 4 * tokens};
+  const bool one = same(kr, vr);
+  if ((overlap(kh, kr) && !same(kh, kr)) || (overlap(kh, vr) && !(one && same(kh, vr))) || (overlap(vh, vr) && !same(vh, vr)) ||
+      (overlap(vh, kr) && !(one && same(vh, kr))) || (overlap(kh, vh) && !(one && same(kh, vh))))
+    return SSQ_EINVAL;
+  for (const RowSpan& x : {kr, vr, kh, vh, places})
+    if (overlap(cached, x)) return SSQ_EINVAL;
+  if (overlap(kh, places) || overlap(vh, places)) return SSQ_EINVAL;
   const ssq::Kv4Store<T> a = {{k, k_stride}, {v, v_stride}, {k_held, k_held_stride}, {v_held, v_held_stride}, slots, cache, tokens, pages, kv_heads, shift_of(page_size)};
   return status_of(ssq::launch_kv4_store(a, head_dim, stream));
 }

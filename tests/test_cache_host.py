@@ -60,6 +60,25 @@ def test_store_refuses_what_no_launch_holds():
     assert call("ssq_kv4_store", STORE, {**given, "head_dim": 64, "tokens": (1 << 25) - 32}) == EALIGN
 
 
+K_AT, ROW, CACHE_BYTES = at(0).value, 2 * 64 * 2, 5 * 2 * 2 * 16 * 36            # of STORE: 4 rows of 256 bytes, the cache
+
+
+@pytest.mark.parametrize("given", [
+    # written rows over rows that are read: moved by a part of a row, by whole rows, in other strides, between the rows and reaching into them
+    dict(k_held=off(16)), dict(k_held=off(ROW)), dict(k_held=off(-3 * ROW)), dict(v_held=off(1 << 20), v_held_stride=136), dict(k_held=at(1)), dict(v_held=at(0)),
+    dict(k_stride=384, k_held=off(1536 + 240), k_held_stride=384), dict(k_stride=1024, k_held=off(ROW), k_held_stride=680), dict(k_held=off(3 * ROW + 240)),
+    dict(k=at(1), v=at(1), k_held=at(1), v_held=off((1 << 20) + 16)),
+    # the two outputs
+    dict(v_held=at(4)), dict(v_held=off((4 << 20) + 16)), dict(k_stride=384, v_stride=384, k_held_stride=384, v_held_stride=384, v_held=off((4 << 20) + 240)),
+    dict(k=at(1), v=at(1), k_held=at(4), v_held=at(4), v_held_stride=256),
+    # the cache and the slots
+    dict(cache=at(0)), dict(cache=off((1 << 20) + 3 * ROW)), dict(cache=at(4)), dict(cache=off((5 << 20) - CACHE_BYTES + 16)), dict(slots=off((3 << 20) + 32)),
+    dict(slots=off((3 << 20) - 12)), dict(slots=off((4 << 20) + 60)), dict(slots=off((5 << 20) - 4)), dict(slots=off((3 << 20) + CACHE_BYTES - 4)),
+])
+def test_store_refuses_outputs_over_other_arrays(given):
+    assert call("ssq_kv4_store", STORE, given) == EINVAL == call("ssq_kv4_store_f32", STORE, given), given
+
+
 DECODE = dict(q=at(0), q_stride=512, requests=2, fresh=1, q_heads=8, kv_heads=2, head_dim=64, scale=0.125, cache=at(1), pages=5, page_size=16, table=at(2),
               table_stride=3, lens=at(3), max_len=40, prefix=0, out=at(4), out_stride=512, workspace=None, workspace_bytes=0, stream=None)
 

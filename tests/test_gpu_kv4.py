@@ -162,6 +162,35 @@ def test_store_in_place_and_into_strided_rows(dtype):
     assert ssq.ssq_kv4_store(k[:0], v[:0], slots[:0], cache) is None and torch.equal(ssq.ssq_kv4_store(k[:0], v[:0], slots[:0], cache, held=True)[0], k[:0])
 
 
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_store_rows_between_each_other(dtype):
+    """Rows of all four arrays in one buffer, in equal and in different strides; keys that are the values, in place."""
+    t, heads, dim, page = 9, 2, 64, 16
+    k, v = (A.model_like(gen(635 + i), (t, heads, dim), dtype) for i in range(2))
+    slots = torch.arange(t, device="cuda", dtype=torch.int32)
+    cache = new_cache(1, heads, page, dim)
+    want = ssq.ssq_kv4_store(k, v, slots, cache, held=True)
+    cells = torch.full((12 * t, heads, dim), 7.0, dtype=dtype, device="cuda")
+    # first cell and step of k, v, k_held, v_held; the last ones in place
+    for places in (((0, 4), (1, 4), (2, 4), (3, 4)), ((3, 4), (2, 4), (1, 4), (0, 4)), ((0, 8), (2, 8), (1, 4), (3, 4)), ((1, 2), (60, 1), (0, 6), (25, 2)),
+                   ((5, 4), (4, 6), (5, 4), (4, 6))):
+        cells.fill_(7.0)
+        rows = [cells[a:a + t * s:s] for a, s in places]
+        rows[0].copy_(k), rows[1].copy_(v)
+        seen = [set(range(a, a + t * s, s)) for a, s in places]
+        if places[0] != places[2]:
+            assert sum(map(len, seen)) == len(set.union(*seen)), "the places are apart"
+        other = new_cache(1, heads, page, dim)
+        ssq.ssq_kv4_store(rows[0], rows[1], slots, other, held=(rows[2], rows[3]))
+        assert torch.equal(rows[2], want[0]) and torch.equal(rows[3], want[1]) and torch.equal(other, cache), places
+        rest = [i for i in range(len(cells)) if i not in set.union(*seen)]
+        assert (cells[rest] == 7).all()
+    both = ssq.ssq_kv4_store(k, k, slots, cache, held=True)
+    same = k.clone()
+    ssq.ssq_kv4_store(same, same, slots, other, held=(same, same))
+    assert torch.equal(both[0], both[1]) and torch.equal(same, both[0]) and torch.equal(cache, other)
+
+
 # --- decoding -----------------------------------------------------------------------------------
 
 def kv4_inputs(lens, fresh, prefix, page, heads, dtype, seed, extra=0):

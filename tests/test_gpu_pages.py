@@ -129,6 +129,58 @@ def test_collect_and_compact(i):
     assert torch.equal(after[0], got[1]) and torch.equal(after[1], got[2])      # the lists after the moves
 
 
+LARGE = [
+    # as POOLS; past 2048 requests or 131072 pages, where marks, counts, lists and moves are launches of their own
+    (2049, 40, 16, 3, 0, 0), (2049, 40, 16, 0, 30, 0.2), (2049, 20, 16, 2, 17, 0), (2049, 60, 16, 4, 4095, 0.01), (2049, 300, 16, 5, 4096, 0.4), (2049, 60, 16, 4, 4097, 0.3),
+    (2500, 60, 16, 4, 9000, 0.05), (2049, 33, 16, 3, 40000, 1.0), (3000, 2000, 16, 130, 140001, 0.3), (40, 500, 16, 1030, 131073, 0.02), (1, 16, 16, 1, 131073, 0),
+    # at the borders of the launch that has all marks in LDS
+    (2048, 60, 16, 4, 131072, 0.1), (2048, 200, 64, 9, 131071, 0), (7, 9000, 16, 2340, 131072, 0.9),
+]
+
+
+@pytest.mark.parametrize("i", range(len(LARGE)))
+def test_collect_and_compact_large_pools(i):
+    requests, longest, page, width, pages, share = LARGE[i]
+    rng = random.Random(890 + i)
+    lens = [rng.randint(-3, longest) for _ in range(requests)]
+    table = [[rng.choice((-1, pages, 2 ** 31 - 1)) if rng.random() < 0.05 else rng.randrange(max(pages, 1)) for _ in range(width)] for _ in lens]
+    pinned = [int(rng.random() < share) * rng.randint(1, 255) for _ in range(pages)] if share else None
+    check_pool(lens, table, page, pages, pinned, width, f"{LARGE[i]}")
+
+
+def check_pool(lens, table, page, pages, pinned, width, tag):
+    dev = [ints(lens), ints(table).view(len(lens), width), page, pages, None if pinned is None else torch.tensor(pinned, dtype=torch.uint8, device="cuda")]
+    ws = torch.full((ssq.ssq_page_collect_workspace_size(pages, True) + 256,), 0xFF, dtype=torch.uint8, device="cuda")
+    same(ssq.ssq_page_collect(*dev, workspace=ws[:-256]), collect_reference(lens, table, page, pages, pinned), f"collect {tag}")
+    got, want = ssq.ssq_page_compact(*dev, workspace=ws[:-256]), compact_reference(lens, table, page, pages, pinned)
+    assert (ws[-256:] == 0xFF).all()
+    same(got[1:], want[1:], f"compact {tag}")
+    assert got[0].flatten().tolist() == sum(want[0], []), f"compact {tag}: table"
+    here = [dev[1].clone(), *(torch.full_like(x, 55) for x in got[1:])]           # the table in place
+    assert all(torch.equal(x, y) for x, y in zip(ssq.ssq_page_compact(dev[0], here[0], *dev[2:], out=here), got)), f"in place {tag}"
+    out = [torch.full_like(x, 55) for x in got[1:3]]
+    after = ssq.ssq_page_collect(dev[0], got[0], page, pages, pinned=dev[4], out=out)
+    assert torch.equal(after[0], got[1]) and torch.equal(after[1], got[2]), f"after the moves {tag}"
+
+
+@pytest.mark.parametrize("held", [0, 1, 4095, 4096, 4097, 8192, 12288])
+@pytest.mark.parametrize("pinned", [False, True])
+def test_compact_where_the_held_pages_end_at_a_block(held, pinned):
+    """As many held pages as whole blocks of 4096, nearly so, none and all: of a pool of three blocks, in any places."""
+    pages, requests = 12288, 2051
+    rng = random.Random(905 + held)
+    ids = rng.sample(range(pages), held)
+    width = max(1, -(-held // requests))
+    table = [(ids[r * width:(r + 1) * width] + [-1] * width)[:width] for r in range(requests)]
+    lens = [16 * width] * requests
+    pins = None
+    if pinned:                                     # of those that requests name
+        pins = [0] * pages
+        for e in ids[::5]:
+            pins[e] = 1
+    check_pool(lens, table, 16, pages, pins, width, f"{held} {pinned}")
+
+
 COPIES = [
     # caches, pages, bytes a page, entries
     (1, 9, 16, 4), (2, 30, 1152, 20), (3, 12, 16400, 5), (65, 8, 4608, 4), (130, 5, 576, 2), (1, 40, 147456, 33), (2, 700, 2304, 900),

@@ -301,6 +301,61 @@ def test_decode_flat_and_sharp_scores(factor, dtype):
     Q.check(run(q, cache, table, lens, 100), *Q.decode_reference(q, cache, 16, table, lens, max(lens), 100), f"factor {factor}")
 
 
+@pytest.mark.parametrize("factor", [4.0, 4096.0])
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("prefix", [0, 100])
+def test_decode_sharp_scores_give_the_winners_value(prefix, dtype, factor):
+    """Keys and values that the grid holds exactly, queries along one key that each sees: all other weights are below
+    e^-200, so that a row is that key's value, whatever the scores' size.  Off by: in bf16 weight times scale rounded and
+    the row rounded (2^-8 each), and codes' offsets in at most 64 terms below 279 scales; in binary32 ten roundings."""
+    fresh, page, (hq, hk, d) = 3, 16, (8, 2, 128)
+    q, cache, table, lens = kv4_inputs([700, 140, 1500], fresh, prefix, page, (hq, hk, d), dtype, 673)
+    g = torch.Generator().manual_seed(674)
+    shape = (cache.shape[0] * page, hk, d // 32, 32)
+    k, v = (torch.randint(-8, 8, shape, generator=g).float() for _ in "kv")
+    for x in (k, v):
+        x.scatter_(3, torch.randint(0, 32, (*shape[:3], 1), generator=g), -8.0)      # the step is 1
+        x *= 1 - 2.0 * torch.randint(0, 2, (*shape[:3], 1), generator=g)             # or -1
+    size = torch.ldexp(torch.ones(()), torch.randint(-6, 7, (*shape[:3], 1), generator=g))
+    k, v, step = k.flatten(2), (v * size).flatten(2), size.expand(shape).flatten(2)
+    held = ssq.ssq_kv4_store(k.to(dtype).cuda(), v.to(dtype).cuda(), torch.arange(shape[0], device="cuda", dtype=torch.int32), cache, held=True)
+    assert torch.equal(held[0].cpu().float(), k) and torch.equal(held[1].cpu().float(), v)
+    want, tol = (torch.zeros(q.shape, dtype=torch.float64) for _ in range(2))
+    for r, n in enumerate(lens):
+        at = torch.arange(n)
+        slot = torch.where(at < prefix, table[0, at // page], table[r, at // page]) * page + at % page
+        for i in range(fresh):
+            seen = n - fresh + i + 1
+            for h in range(hq):
+                kv = h * hk // hq
+                w = (0, seen - 1, max(prefix - 1, 0), int(torch.randint(0, seen, (), generator=g)))[(h + i) % 4]
+                row = factor * k[slot[w], kv]
+                score = (k[slot[:seen], kv].double() * row.double()).sum(1) * d ** -0.5
+                rest = torch.cat((score[:w], score[w + 1:]))
+                assert score[w] - rest.max() > 200
+                q[r, i, h] = row.to(dtype)
+                want[r, i, h] = v[slot[w], kv].double()
+                tol[r, i, h] = 2.0 ** -7 * want[r, i, h].abs() + 64 * 279 * Q.U * step[slot[w], kv] if dtype == BF else 10 * Q.U * want[r, i, h].abs()
+    for ws in (None, torch.empty(0, dtype=torch.uint8, device="cuda")):
+        Q.check(run(q, cache, table, lens, prefix, workspace=ws), want, tol, f"{prefix} {dtype} {factor}")
+
+
+CHUNKS = [
+    # as DECODES: many new tokens at once, whose last tile of rows is partly empty
+    ([400], 150, 0, 16, (8, 2, 64)), ([131], 131, 0, 32, (3, 3, 64)), ([333, 290], 40, 200, 64, (10, 2, 128)), ([20, 200, 90], 130, 0, 16, (4, 4, 64)),
+]
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("i", range(len(CHUNKS)))
+def test_decode_of_many_new_tokens(i, dtype):
+    lens, fresh, prefix, page, heads = CHUNKS[i]
+    q, cache, table, lens = kv4_inputs(lens, fresh, prefix, page, heads, dtype, 676 + i)
+    ref, bound = Q.decode_reference(q, cache, page, table, lens, max(lens), prefix)
+    for ws in (None, torch.empty(0, dtype=torch.uint8, device="cuda")):
+        Q.check(run(q, cache, table, lens, prefix, workspace=ws), ref, bound, f"{CHUNKS[i]} {dtype}")
+
+
 @pytest.mark.parametrize("sign", [1, -1])
 def test_decode_rising_and_falling_scores(sign):
     """Each key outscores all before it by far: the running reference moves at every tile."""

@@ -733,6 +733,11 @@ def _collect_bytes(pages: int, compact: bool) -> int:
     return int(lib().ssq_page_collect_workspace_size(pages, int(compact)))
 
 
+# Bytes of a workspace that lies behind the outputs, in their allocation (1.4 us less of the host than one of its own, of 9 in all
+# for 9000 pages).  A larger one (a compaction of 116000 pages) is freed with the call, not kept by whoever keeps an output.
+_SCRATCH_INSIDE = 1 << 20
+
+
 def _collect(name: str, lens, table, page_size, pages, pinned, sizes, out, workspace, compact: bool):
     """ssq_page_collect or ssq_page_compact into int32 arrays of `sizes`, allocated with the workspace where they are not given."""
     if lens.dim() != 1 or table.dim() != 2:
@@ -745,7 +750,8 @@ def _collect(name: str, lens, table, page_size, pages, pinned, sizes, out, works
         raise ValueError("workspace must be contiguous")
     if out is None:
         total = sum(sizes)
-        scratch = 0 if workspace is not None else -total % 64 + (need + 3) // 4
+        inside = workspace is None and need <= _SCRATCH_INSIDE
+        scratch = -total % 64 + (need + 3) // 4 if inside else 0
         buf = torch.empty(total + scratch, dtype=i32, device=lens.device)
         base = _ptr(buf)
         out = torch.split_with_sizes(buf, (*sizes, scratch))[:-1]
@@ -755,8 +761,10 @@ def _collect(name: str, lens, table, page_size, pages, pinned, sizes, out, works
             at += 4 * size
         if compact:
             out = (out[0].view(n, width), *out[1:])
-        if workspace is None:                   # behind the outputs, from the next 256 bytes on
+        if inside:                              # from the next 256 bytes on
             scratch_at, scratch_bytes = base + 4 * (total + -total % 64), need
+        elif workspace is None:
+            workspace = torch.empty(need, dtype=torch.uint8, device=lens.device)
     else:
         to = [_flat(x, "an output", i32, (n, width) if compact and i == 0 else (size,)) for i, (x, size) in enumerate(zip(out, sizes))]
         if workspace is None:

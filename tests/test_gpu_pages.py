@@ -163,6 +163,16 @@ def check_pool(lens, table, page, pages, pinned, width, tag):
     assert torch.equal(after[0], got[1]) and torch.equal(after[1], got[2]), f"after the moves {tag}"
 
 
+@pytest.mark.parametrize("pages", [300, 116000, 117000, 1000000, 1100000])
+@pytest.mark.parametrize("compact", [False, True])
+def test_outputs_do_not_keep_a_large_workspace(compact, pages):
+    lens, table = ints([20, 33]), ints([[5, 9, 7], [1, 250, 2]])
+    got = (ssq.ssq_page_compact if compact else ssq.ssq_page_collect)(lens, table, 16, pages)
+    own = sum(x.numel() * x.element_size() for x in got)
+    assert all(x.untyped_storage().nbytes() <= own + (1 << 20) + 256 for x in got)
+    same(got, (compact_reference if compact else collect_reference)(lens.tolist(), table.tolist(), 16, pages), f"{pages}")
+
+
 @pytest.mark.parametrize("held", [0, 1, 4095, 4096, 4097, 8192, 12288])
 @pytest.mark.parametrize("pinned", [False, True])
 def test_compact_where_the_held_pages_end_at_a_block(held, pinned):

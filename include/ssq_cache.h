@@ -134,6 +134,7 @@ int ssq_page_fork(const int32_t* parents, int64_t requests, const int32_t* lens,
  * that have ended are left out, or have the length 0.  The list is one for ssq_page_tables and
  * ssq_page_fork, from entry 0 on.
  *
+ *   requests    0 to 2^20 (up to 2048, and up to 131072 pages, in one or three launches instead of four or seven)
  *   lens        device, int32 [requests]; negative values count as 0.  lens and table may be NULL if
  *               requests or table_stride is 0
  *   table       device, int32 [requests, table_stride]; entries outside [0, pages) name none;
@@ -183,7 +184,7 @@ size_t ssq_page_collect_workspace_size(int64_t pages, int compact);
  *               [0, pages) is skipped, as is one of a page to itself
  *   entries     0 to 2^30
  * No page may be named twice in dst, or both in src and in dst (those of ssq_page_fork and
- * ssq_page_compact are not): it would hold a mixture.
+ * ssq_page_compact are not): it would hold a mixture.  No two caches may overlap, but one may be named twice.
  */
 int ssq_page_copy(void* const* caches, int count, int64_t page_bytes, int64_t pages, const int32_t* src,
                   const int32_t* dst, int64_t entries, hipStream_t stream);

@@ -29,11 +29,12 @@
 //
 // Own keys are bound by memory: 96 requests of 8192 keys (908 MB) take 158 us, 5.75 TB/s; reading the
 // same bytes in the same order, without arithmetic, takes 148.  48 requests of 4096 to 8191 keys (337 MB):
-// 72 us, of which 4.7 are the joining launch and the rest ends unevenly.  One request of 16383 keys: 12.2,
+// 71 us, of which 4.8 are the joining launch and the rest ends unevenly.  One request of 16383 keys: 12.1,
 // of which 3.4 are the joining launch; the walk's 9 are a launch, four loads that wait for each other and
-// four tiles.  The prefix is bound by the vector unit: 16 rows and 32 keys take about 170
-// instructions, a third of which unpack (shared by two tiles of rows) and half of which apply scales,
-// beside 24 products: 64 requests of 1 to 1024 keys behind 8192 take 34.5 us (50 MB, 9.2 GFLOP).
+// four tiles.  On a prefix 16 rows and 32 keys take about 170 instructions, a third of which unpack (shared
+// by two tiles of rows) and half of which apply scales, beside 24 products: 64 requests of 1 to 1024 keys
+// behind 8192 take 34.5 us (50 MB, 9.2 GFLOP), in which vector instructions have 45 % of the SIMDs' cycles and
+// products 17 %; the rest is waiting and the uneven end.
 #include "attention_join.h"
 #include "kv4.h"
 
@@ -63,10 +64,19 @@ int64_t steps_of(int64_t keys, int parts) { return ceil_div(ceil_div(keys, parts
 
 // Parts of the requests' own keys where no prefix is shared, for `groups` workgroups a part: the quickest by a fit
 // of its time (us).  A step of 128 keys takes a workgroup 1.1 where it has a CU to itself, two beside each other
-// 1.8, three 2.35, and a CU full of them 0.8 each; parts have to be joined, by a launch of 3 and their traffic.  1 request of 16383 keys (8
-// key/value heads): 32 parts 12.3 us, 16 15.0, 64 13.7; 16 of 1024: 1 part 12.3, 4 parts 12.2, 8 parts 13.1; 32 of
-// 4096: 1 part 42.0, 2 parts 38.2, 3 parts 35.2, 8 parts 39.5; 48 of 4096 to 8191: 1 part 101, 2 parts 73, 4 parts 78; 64 of 1024:
-// 1 part 16.6, 2 parts 20.7.
+// 1.8, three 2.35, and a CU full of them 0.8 each; parts have to be joined, by a launch of 3 and their traffic.  These
+// constants were read on an earlier state of the walk, with up to 8 rows in bf16; what they choose was read again on
+// this one, with the other forms (8 key/value heads, us, * the choice; the best is at most 7 % quicker):
+//   1 request of 16383 keys          16, 24, 32*, 48, 64 parts 15.0, 13.5, 12.2, 13.6, 13.6
+//   16 of 1024                       1, 2, 4*, 8 parts         12.0, 12.0, 11.9, 12.7
+//   32 of 4096                       1, 2, 3*, 4, 8 parts      35.6, 30.6, 31.3, 31.7, 35.4
+//   48 of 4096 to 8191               1, 2*, 3, 4, 6, 8 parts   78.5, 71.4, 76.9, 76.2, 76.0, 76.5
+//   64 of 1024                       1*, 2, 4 parts            16.6, 20.1, 23.0
+//   32 of 4096, 4 tokens (16 rows)   1, 2, 3*, 4 parts         38.2, 34.2, 36.4, 40.0
+//   32 of 4096, 8 tokens (32 rows)   1*, 2, 3, 4 parts         49.7, 48.1, 54.9, 58.4
+//   1 of 8704, 512 tokens            1, 2*, 4, 8 parts         138, 149, 163, 191
+//   binary32: 1 of 16383             16, 32*, 64 parts         30.1, 21.2, 22.5
+//   binary32: 48 of 4096 to 8191     1, 2*, 3, 4, 8 parts      257, 172, 183, 174, 182
 int choose_parts(int64_t groups, int64_t keys, int64_t line_rows) {
   int best = 1;
   double best_us = 0.0;
@@ -82,8 +92,11 @@ int choose_parts(int64_t groups, int64_t keys, int64_t line_rows) {
 
 // The same beside a prefix, whose workgroups take 1.3 for a step of 128 keys and 32 rows, 2.3 where a CU has two of
 // them, and in between where it has work on own keys too; a CU that is full does a step in 1.15, one of a
-// request's own keys in 0.8.  Together: the work, or the longest workgroup.  64 requests of one key behind 8192 (256 rows, 8 key/value heads): 4 parts 31.7 us, 6 parts 34.2, 8
-// parts 31.9; behind 16384: 50.8, 54.1, 44.2; of 1 to 1024 keys behind 8192, undivided: 34.5, 37.9, 40.1.
+// request's own keys in 0.8.  Together: the work, or the longest workgroup.  64 requests of one key behind 8192 (256 rows, 8 key/value
+// heads): 2, 3, 4 (the choice), 6, 8 parts 49.7, 37.9, 31.2, 33.9, 31.2 us; behind 16384: 4, 6, 8 (the choice), 12 parts
+// 51.0, 54.5, 44.2, 49.1; of 1 to 1024 keys behind 8192, undivided: 3, 4 (the choice), 6, 8 parts 39.8, 35.0, 38.4, 40.7.  Binary32
+// goes by the same: 16 requests of 4 tokens and 4 to 700 keys behind 1000 take 11.3 in 8 parts and 4 of their own (the
+// choice), 12.4 in 4 and 2, 13.9 in 8 and 1, 15.2 in 2 and 1.
 void choose_shared_parts(Kv4Plan& p, int64_t requests, int kv_heads, int64_t prefix, int64_t behind) {
   const int64_t wide = (int64_t)p.prefix_tiles * kv_heads, own = requests * p.own_tiles * kv_heads;
   double best_us = 0.0;

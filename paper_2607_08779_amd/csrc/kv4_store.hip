@@ -5,9 +5,9 @@
 // four threads a group, whose maxima they exchange in DPP moves.
 //
 // Long runs are bound by the rows' bytes: 4099 tokens of 8 heads of 128 with the rows as held (38 MB)
-// 10.3 us, of which a copy of as many bytes takes 7.3 and the launch 2; all loads, then all stores are under way
+// 10.2 us, of which a copy of as many bytes takes 7.4 and the launch 2; all loads, then all stores are under way
 // together.  With a division for each element and tokens of a head spread over workgroups it was 12.7.
-// One token takes 2.8, the launch.
+// In binary32, which divides for each element, they take 18.5 (72 MB: a copy 13.8).  One token takes 2.8, the launch.
 #include "kv4.h"
 #include "mfma_dequant.h"
 

@@ -6,8 +6,8 @@
 // bound them.  Fork is one launch: every workgroup finds for itself how many pages the rows before its
 // own take, as page_tables.hip does (64 rows 3.9 us, 1024 rows of 512 pages 5.7).  Collect and compact mark held
 // pages, count them and write lists whose places follow from the counts (64 requests, 9000 pages 8.7 us;
-// compacting 98000 pages of 512 requests 13.7).  A copy is bound by the pages' bytes, read and written (939 MB 165 us,
-// 5.7 TB/s).  Nothing depends on the order in which workgroups or atomics run.
+// compacting 98000 pages of 512 requests 13.7, 140000 pages 31.8).  A copy is bound by the pages' bytes, read and written (939 MB 167 us,
+// 5.6 TB/s).  Nothing depends on the order in which workgroups or atomics run.
 #include "page_lists.h"
 
 namespace ssq {
@@ -317,7 +317,7 @@ __global__ __launch_bounds__(kThreads) void rename_kernel(const PageCollect a, c
   }
 }
 
-// Pools of up to 131072 pages: every workgroup has all marks, in bits in LDS, and counts them for itself; then each takes
+// Pools of up to 131072 pages and 2048 requests: every workgroup has all marks, in bits in LDS, and counts them for itself; then each takes
 // its share of the lists and rows.  The marks of a small table every workgroup makes for itself, in the only launch
 // (64 requests, 9000 pages: 10.4 us in the launches above, 8.6 so).  Where the table is larger, atomics on LDS at
 // random places would take longer than marking in memory in launches of its own (compacting 98000 pages of 512
@@ -538,8 +538,8 @@ struct Arrays {
   uint8_t* p[kCopyArrays];
 };
 
-// A row of the grid is an array.  Streaming loads and stores of small chunks: 200 pages of 73 KB in 32 arrays (939 MB read and
-// written) 156 us, 161 with cached ones, 160 and 169 in chunks of 16 KB.
+// A row of the grid is an array.  Streaming loads and stores of small chunks: 199 pages of 74 KB in 32 arrays (939 MB read and
+// written) 167 us, 180 with cached ones, 168 to 171 and 181 in chunks of 16 KB.
 __global__ __launch_bounds__(kThreads) void page_copy_kernel(const Arrays arrays, const int32_t* src, const int32_t* dst, int64_t entries,
                                                              int64_t pages, int64_t page_bytes, uint32_t chunks) {
   const uint32_t first = blockIdx.x / chunks, chunk = blockIdx.x - first * chunks;

@@ -781,7 +781,8 @@ def ssq_page_collect(lens: torch.Tensor, table: torch.Tensor, page_size: int, pa
                      out=None, workspace: Optional[torch.Tensor] = None):
     """The pages of a pool of ``pages`` that no request holds, on the current stream: request r holds the
     first ceil(lens[r] / page_size) entries of ``table[r]`` (int32 [requests, pages]); ``pinned`` (uint8 [pages])
-    is not 0 for pages that are held in any case.  Returns (free_pages [pages], ascending, then -1; count [1]), int32.
+    is not 0 for pages that are held in any case.  Returns (free_pages [pages], ascending, then -1; count [1]), int32,
+    in one allocation.
     ``out`` = these two reuses buffers; ``workspace`` (uint8, any contents, ``ssq_page_collect_workspace_size`` bytes)
     is allocated where it is not given."""
     return _collect("ssq_page_collect", lens, table, page_size, pages, pinned, (pages, 1), out, workspace, False)
@@ -804,7 +805,8 @@ def ssq_page_collect_workspace_size(pages: int, compact: bool = False) -> int:
 def ssq_page_copy(caches, src: torch.Tensor, dst: torch.Tensor) -> None:
     """Page ``src[i]`` of every cache into its page ``dst[i]`` (int32; negative: nothing), on the current stream.
     ``caches``: contiguous tensors [pages, ...] of one device whose pages have the same number of bytes, such as
-    all layers' k_pages and v_pages, or their 4-bit caches.  No page may be named twice in dst, or in both."""
+    all layers' k_pages and v_pages, or their 4-bit caches; they must not overlap.  No page may be named twice in dst,
+    or in both."""
     caches = list(caches)
     if not caches:
         return
